@@ -442,6 +442,82 @@ GF_API gf_status_t gf_c2_decay_logit(const void *x, const void *x_prev, const fl
 GF_API gf_status_t gf_gold_key_compress(const void *x, const void *w_kd, void *c, long long rows, int D, int Dc,
                                  gf_stream_t stream);
 
+/* Gradient of gf_c2_layernorm: with mu, rstd = 1 / sqrt(var + eps) of the row, xhat = (y - mu) rstd and g = dout * gamma,
+ *     dy[c] = rstd (g[c] - mean(g) - xhat[c] mean(g xhat)),   dgamma[c] = sum_rows dout[c] xhat[c],   dbeta[c] = sum_rows dout[c].
+ *   y, dout, dy   DEVICE [rows][H][N] (bf16, resp. fp32 for _f32), 16-byte aligned; y is the forward call's INPUT (its statistics
+ *                 are taken again: the forward call keeps nothing); dy may be y or dout (in place)
+ *   gamma         DEVICE fp32 [H*N] or NULL for 1;  dgamma, dbeta  DEVICE fp32 [H*N], each written, or NULL where not wanted
+ *   workspace     DEVICE, gf_c2_layernorm_backward_workspace_bytes(H,N) bytes, 16-byte aligned (GF_ERR_WORKSPACE if absent or too
+ *                 small; NULL will do where neither dgamma nor dbeta is wanted)
+ * Arithmetic and sums in fp32, in an order that the sizes and the GPU alone decide (no atomics); dy is rounded once.  H*N as for
+ * gf_c2_layernorm.  rows = 0 writes zeros to dgamma and dbeta.  Enqueues two kernels on `stream` (one without dgamma and
+ * dbeta), allocates nothing, does not synchronise. */
+GF_API gf_status_t gf_c2_layernorm_backward(const void *y, const float *gamma, float eps, const void *dout, void *dy,
+                                     float *dgamma, float *dbeta, long long rows, int H, int N, void *workspace,
+                                     size_t workspace_bytes, gf_stream_t stream);
+GF_API gf_status_t gf_c2_layernorm_backward_f32(const float *y, const float *gamma, float eps, const float *dout,
+                                         float *dy, float *dgamma, float *dbeta, long long rows, int H, int N,
+                                         void *workspace, size_t workspace_bytes, gf_stream_t stream);
+GF_API size_t gf_c2_layernorm_backward_workspace_bytes(int H, int N);
+
+/* The gated linear block of the channel mix and of gated hidden layers:
+ *     y = act(x W) * (x2 W2)          elementwise;  without W2:  y = act(x W).
+ * The paper's channel mix (channel-mix equations) is h = relu(x_k W_k)^2 (GF_ACT_RELU2, no W2) followed by
+ * o = sigmoid(x_r W_r) * (h W_v) (GF_ACT_SIGMOID, x2 = h, W2 = W_v).
+ *   x    DEVICE bf16 [rows][K1]        w    DEVICE bf16 [K1][F] row-major
+ *   w2   DEVICE bf16 [K2][F], or NULL: no second factor (then x2 is NULL and K2 is 0)
+ *   x2   DEVICE bf16 [rows][K2], or NULL: x itself (then K2 is K1)
+ *   y    DEVICE bf16 [rows][F], written; must not be one of the inputs
+ *   act  gf_act_t: sigmoid; relu(a)^2; silu, a sigmoid(a); gelu, a Phi(a) with the normal distribution Phi
+ * Both products on the tensor cores with fp32 accumulation, activation and product in fp32, one rounding to bf16.  K1, K2 and
+ * F are multiples of 8 (GF_ERR_UNSUPPORTED otherwise); pointers 16-byte aligned; rows = 0 is a no-op.  Enqueues one kernel on
+ * `stream`, allocates nothing, does not synchronise. */
+typedef enum gf_act { GF_ACT_SIGMOID = 0, GF_ACT_RELU2 = 1, GF_ACT_SILU = 2, GF_ACT_GELU = 3 } gf_act_t;
+GF_API gf_status_t gf_gated_linear(const void *x, const void *w, const void *x2, const void *w2, int act, void *y,
+                            long long rows, int K1, int K2, int F, gf_stream_t stream);
+
+/* Gradient of gf_gated_linear.  With a = x W, b = x2 W2 (computed again from the inputs), da = dy b act'(a), db = dy act(a):
+ *     dx = da W^T,   dw = x^T da,   dx2 = db W2^T,   dw2 = x2^T db;   with x2 = NULL, dx = da W^T + db W2^T.
+ *   x, w, x2, w2, act, sizes   as for gf_gated_linear;   dy  DEVICE bf16 [rows][F]
+ *   dx [rows][K1], dw [K1][F], dx2 [rows][K2], dw2 [K2][F]   DEVICE bf16, written; dw2 is NULL without w2, dx2 without x2; none may
+ *                 be an input or another output
+ *   workspace     DEVICE, gf_gated_linear_backward_workspace_bytes(rows,F,w2 != NULL) bytes, 16-byte aligned (da and db);
+ *                 GF_ERR_WORKSPACE if absent or too small
+ * relu^2 has derivative 0 at 0.  da and db are rounded to bf16 (they are operands of the second products), sums are fp32, results
+ * rounded once; no atomics.  rows = 0 writes zeros to dw and dw2.  Enqueues two kernels on `stream`, allocates nothing, does not
+ * synchronise. */
+GF_API gf_status_t gf_gated_linear_backward(const void *x, const void *w, const void *x2, const void *w2, int act,
+                                     const void *dy, void *dx, void *dw, void *dx2, void *dw2, long long rows, int K1,
+                                     int K2, int F, void *workspace, size_t workspace_bytes, gf_stream_t stream);
+GF_API size_t gf_gated_linear_backward_workspace_bytes(long long rows, int F, int gated);
+
+/* Cross entropy of a linear layer over the vocabulary, without keeping the logits.  For every row
+ *     z = x W^T,   lse = log sum_v exp(z[v]),   loss = lse - z[target].
+ *   x        DEVICE bf16 [rows][D]      w  DEVICE bf16 [V][D] row-major (one row per entry of the vocabulary)
+ *   targets  DEVICE int64 [rows]; one outside 0 .. V-1 means that the row has none: its loss is 0
+ *   loss, lse  DEVICE fp32 [rows], written (lse is what the gradient takes)
+ *   workspace  DEVICE, gf_vocab_loss_workspace_bytes(rows,V) bytes, 16-byte aligned; GF_ERR_WORKSPACE if absent or too small
+ * bf16 operands on the tensor cores, fp32 logits and sums of exponentials of differences to a running maximum.  D is a multiple of 8
+ * (GF_ERR_UNSUPPORTED otherwise), V any positive number.  An infinite or NaN logit has the effect it has in the formula.
+ * rows = 0 is a no-op.  Enqueues two kernels on `stream`, allocates nothing, does not synchronise. */
+GF_API gf_status_t gf_vocab_loss(const void *x, const void *w, const int64_t *targets, float *loss, float *lse,
+                          long long rows, int D, long long V, void *workspace, size_t workspace_bytes,
+                          gf_stream_t stream);
+GF_API size_t gf_vocab_loss_workspace_bytes(long long rows, long long V);
+
+/* Gradient of gf_vocab_loss: with P[t][v] = (exp(z[t][v] - lse[t]) - [v is the target of t]) dloss[t], and 0 in rows without a
+ * target,    dx = P W,   dw = P^T x.
+ *   x, w, targets, sizes   as for gf_vocab_loss, lse what it wrote;   dloss  DEVICE fp32 [rows], or NULL for 1 in every row
+ *   dx [rows][D], dw [V][D]   DEVICE bf16, written; neither may be an input
+ *   workspace  DEVICE, gf_vocab_loss_backward_workspace_bytes(rows,D,V) bytes, 16-byte aligned; GF_ERR_WORKSPACE if absent or
+ *              too small (256 MB for a piece of P, 2 KB per row at least; fp32 sums of dx where the vocabulary takes several pieces)
+ * P is rounded to bf16 (it is an operand of both products), sums are fp32, results rounded once; no atomics.  rows = 0 writes zeros to
+ * dw.  Enqueues two kernels per piece of the vocabulary on `stream`, allocates nothing, does not synchronise. */
+GF_API gf_status_t gf_vocab_loss_backward(const void *x, const void *w, const int64_t *targets, const float *lse,
+                                   const float *dloss, void *dx, void *dw, long long rows, int D, long long V,
+                                   void *workspace, size_t workspace_bytes, gf_stream_t stream);
+GF_API size_t gf_vocab_loss_backward_workspace_bytes(long long rows, int D, long long V);
+
 GF_API int gf_wkv6_version(void);
 
 #ifdef __cplusplus

@@ -339,3 +339,84 @@ def rel_l2(a, b) -> float:
     den = float(np.linalg.norm(b))
     num = float(np.linalg.norm(a - b))
     return num / den if den > 0 else num
+
+
+# ---- the operators around the recurrence, from their formulas in float64 (numpy; no code shared with the library)
+def _np64(a):
+    if a is None:
+        return None
+    if hasattr(a, "detach"):
+        a = a.detach().cpu().double().numpy()
+    return np.asarray(a, dtype=np.float64)
+
+
+def layernorm_heads_backward(y, dout, gamma=None, eps=1e-5):
+    """Gradient of layernorm_heads() over the last two axes: (dy, dgamma [H*N], dbeta [H*N])."""
+    y, dout, gamma = _np64(y), _np64(dout), _np64(gamma)
+    shape = y.shape
+    D = shape[-2] * shape[-1]
+    y, dout = y.reshape(-1, D), dout.reshape(-1, D)
+    c = y - y.mean(1, keepdims=True)
+    rstd = 1 / np.sqrt((c * c).mean(1, keepdims=True) + eps)
+    xhat = c * rstd
+    g = dout if gamma is None else dout * gamma.reshape(D)
+    dy = rstd * (g - g.mean(1, keepdims=True) - xhat * (g * xhat).mean(1, keepdims=True))
+    return dy.reshape(shape), (dout * xhat).sum(0), dout.sum(0)
+
+
+def activation(a, act):
+    """(value, derivative) of one of the gated linear block's activations."""
+    from scipy.special import expit, ndtr
+    a = _np64(a)
+    if act == "relu2":
+        return np.maximum(a, 0) ** 2, 2 * np.maximum(a, 0)
+    if act == "gelu":
+        return a * ndtr(a), ndtr(a) + a * np.exp(-a * a / 2) / np.sqrt(2 * np.pi)
+    s = expit(a)
+    if act == "sigmoid":
+        return s, s * expit(-a)
+    assert act == "silu"
+    return a * s, s * (1 + a * expit(-a))
+
+
+def gated_linear(x, w, x2=None, w2=None, act="silu"):
+    """act(x w) * (x2 w2); without w2 act(x w), without x2 both of x.  x: [rows, K1]."""
+    x, w, x2, w2 = (_np64(t) for t in (x, w, x2, w2))
+    f = activation(x @ w, act)[0]
+    return f if w2 is None else f * ((x if x2 is None else x2) @ w2)
+
+
+def gated_linear_backward(x, w, dy, x2=None, w2=None, act="silu"):
+    """Gradient of gated_linear(): (dx, dw, dx2, dw2), None where there is no such input."""
+    x, w, dy, x2, w2 = (_np64(t) for t in (x, w, dy, x2, w2))
+    f, df = activation(x @ w, act)
+    if w2 is None:
+        da = dy * df
+        return da @ w.T, x.T @ da, None, None
+    v = x if x2 is None else x2
+    da, db = dy * (v @ w2) * df, dy * f
+    dx, dv, dw, dw2 = da @ w.T, db @ w2.T, x.T @ da, v.T @ db
+    return (dx + dv, dw, None, dw2) if x2 is None else (dx, dw, dv, dw2)
+
+
+def vocab_loss(x, w, targets):
+    """(loss, lse) of the logits x w^T; loss 0 where the target lies outside the vocabulary.  x: [rows, D], w: [V, D]."""
+    z = _np64(x) @ _np64(w).T
+    t = np.asarray(targets.cpu() if hasattr(targets, "cpu") else targets)
+    top = z.max(1)
+    lse = top + np.log(np.exp(z - top[:, None]).sum(1))
+    has = (t >= 0) & (t < z.shape[1])
+    return np.where(has, lse - z[np.arange(len(t)), np.where(has, t, 0)], 0.0), lse
+
+
+def vocab_loss_backward(x, w, targets, dloss=None):
+    """Gradient of sum(dloss * loss): (dx, dw, P) with P the gradient of the logits."""
+    x, w, dloss = _np64(x), _np64(w), _np64(dloss)
+    z = x @ w.T
+    t = np.asarray(targets.cpu() if hasattr(targets, "cpu") else targets)
+    P = np.exp(z - z.max(1, keepdims=True))
+    P /= P.sum(1, keepdims=True)
+    has = (t >= 0) & (t < z.shape[1])
+    P[np.nonzero(has)[0], t[has]] -= 1
+    P *= (has if dloss is None else np.where(has, dloss, 0.0))[:, None]
+    return P @ w, P.T @ x, P

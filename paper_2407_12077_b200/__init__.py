@@ -20,6 +20,7 @@ from . import _build
 __all__ = [
     "GfError", "load_library", "library_path", "prefill", "prefill_varlen", "step", "bind_step",
     "sequence_summary", "fold_summaries", "SUMMARY_FLOATS", "backward", "backward_c2", "prefill_train", "backward_workspace_bytes", "backward_varlen", "backward_varlen_workspace_bytes", "prefill_varlen_train", "decay_logit", "prefill_c2", "prefill_varlen_c2", "step_c2", "prefill_static", "STATIC_SCRATCH_BYTES", "prefill_host", "host_workspace_bytes", "workspace_bytes", "split_plan", "set_workspace", "set_kernel", "last_device_status",
+    "layernorm_heads", "layernorm_heads_backward", "key_compress", "gated_linear", "gated_linear_backward", "ACTIVATIONS", "vocab_loss", "vocab_loss_backward",
     "launch_count", "status_string", "version", "set_wait_limit", "selftest_wait_timeout",
     "KERNEL_AUTO", "KERNEL_EXACT", "KERNEL_CHUNKED",
 ]
@@ -32,7 +33,7 @@ _native = None               # the binding's C++ part (csrc/binding.cpp), once t
 _NATIVE_FNS = ("gf_wkv6_prefill", "gf_wkv6_prefill_f32", "gf_wkv6_prefill_c2", "gf_wkv6_prefill_varlen", "gf_wkv6_prefill_varlen_f32",
                "gf_wkv6_prefill_varlen_c2", "gf_wkv6_step", "gf_wkv6_step_f32", "gf_wkv6_step_c2", "gf_c2_layernorm", "gf_c2_layernorm_f32",
                "gf_gold_key_compress", "gf_wkv6_workspace_bytes")
-_vp, _i, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+_vp, _i, _sz, _ll = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_longlong
 
 # name -> (restype, argtypes); the single place the ABI is mirrored in Python
 _SIGNATURES = {
@@ -73,6 +74,16 @@ _SIGNATURES = {
     "gf_c2_layernorm_f32": (_i, [_vp, _vp, _vp, ctypes.c_float, _vp, ctypes.c_longlong, _i, _i, _vp]),
     "gf_gold_key_compress": (_i, [_vp, _vp, _vp, ctypes.c_longlong, _i, _i, _vp]),
     "gf_c2_decay_logit": (_i, [_vp] * 10 + [_i] * 5 + [_vp]),
+    "gf_c2_layernorm_backward": (_i, [_vp, _vp, ctypes.c_float] + [_vp] * 4 + [_ll, _i, _i, _vp, _sz, _vp]),
+    "gf_c2_layernorm_backward_f32": (_i, [_vp, _vp, ctypes.c_float] + [_vp] * 4 + [_ll, _i, _i, _vp, _sz, _vp]),
+    "gf_c2_layernorm_backward_workspace_bytes": (_sz, [_i, _i]),
+    "gf_gated_linear": (_i, [_vp] * 4 + [_i, _vp, _ll] + [_i] * 3 + [_vp]),
+    "gf_gated_linear_backward": (_i, [_vp] * 4 + [_i] + [_vp] * 5 + [_ll] + [_i] * 3 + [_vp, _sz, _vp]),
+    "gf_gated_linear_backward_workspace_bytes": (_sz, [_ll, _i, _i]),
+    "gf_vocab_loss": (_i, [_vp] * 5 + [_ll, _i, _ll, _vp, _sz, _vp]),
+    "gf_vocab_loss_workspace_bytes": (_sz, [_ll, _ll]),
+    "gf_vocab_loss_backward": (_i, [_vp] * 7 + [_ll, _i, _ll, _vp, _sz, _vp]),
+    "gf_vocab_loss_backward_workspace_bytes": (_sz, [_ll, _i, _ll]),
     "gf_wkv6_set_kernel": (_i, [_i]),
     "gf_wkv6_last_device_status": (_i, [_vp]),
     "gf_wkv6_set_wait_limit": (_i, [ctypes.c_uint]),
@@ -631,6 +642,138 @@ def key_compress(x, w_kd, out=None, stream=None):
         _check(lib.gf_gold_key_compress(_dev(x, "x", bf), _dev(w_kd, "w_kd", bf), c_ptr,
                                         rows, D, Dc, _stream(stream)), "gf_gold_key_compress")
     return out
+
+
+def _one_device(**tensors) -> None:
+    """Every tensor of a call lives on one device (the launch goes to that of the first)."""
+    there = {n: t.device for n, t in tensors.items() if t is not None}
+    if len(set(there.values())) > 1:
+        raise ValueError("tensors of one call on different devices: " + ", ".join(f"{n} on {d}" for n, d in there.items()))
+
+
+def layernorm_heads_backward(y, dout, gamma=None, eps=1e-5, want_params=True, dy=None, stream=None, workspace=None):
+    """gf_c2_layernorm_backward(_f32): gradient of layernorm_heads().  y (the forward call's input), dout: [..., H, N] CUDA
+    tensors of one dtype (bf16 or fp32, contiguous); gamma: fp32 [H*N] (or [H, N]) or None.  Returns (dy, dgamma, dbeta), the
+    latter two fp32 [H*N] (None unless want_params).  dy defaults to a new tensor (y or dout: in place); the workspace, unless a
+    uint8 tensor of enough bytes is passed, is allocated here."""
+    lib = _lib or load_library()
+    H, N = y.shape[-2:]
+    D = H * N
+    rows = y.numel() // D if D else 0
+    dt, f32 = y.dtype, torch.float32
+    sfx = _suffix(dt)
+    _one_device(y=y, dout=dout, gamma=gamma, dy=dy, workspace=workspace)
+    ins = [_dev(y, "y"), _dev(None if gamma is None else gamma.reshape(D), "gamma", f32), float(eps), _dev(dout, "dout", dt, y.shape)]
+    if dy is None:
+        dy = torch.empty_like(y)
+    dgamma = dbeta = ws = None
+    with _on(y):
+        if want_params:
+            dgamma, dbeta = torch.empty((2, D), device=y.device, dtype=f32).unbind()
+            nbytes = int(lib.gf_c2_layernorm_backward_workspace_bytes(H, N))
+            ws = workspace if workspace is not None and workspace.numel() >= nbytes else torch.empty(max(nbytes, 16), dtype=torch.uint8, device=y.device)
+        _check(getattr(lib, "gf_c2_layernorm_backward" + sfx)(
+            *ins, _dev(dy, "dy", dt, y.shape), _dev(dgamma, "dgamma"), _dev(dbeta, "dbeta"), rows, H, N, _dev(ws, "workspace"),
+            0 if ws is None else ws.numel(), _stream(stream)), "gf_c2_layernorm_backward" + sfx)
+    return dy, dgamma, dbeta
+
+
+ACTIVATIONS = {"sigmoid": 0, "relu2": 1, "silu": 2, "gelu": 3}       # gf_act_t
+
+
+def _gated_args(x, w, x2, w2, act):
+    """Device pointers and sizes of a gated linear block's inputs: (pointers, activation, (rows, K1, K2, F))."""
+    bf = torch.bfloat16
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}, got {act!r}")
+    K1, F = w.shape
+    K2 = 0
+    if w2 is None:
+        if x2 is not None:
+            raise ValueError("x2 without w2")
+    else:
+        K2 = w2.shape[0]
+        _dev(w2, "w2", bf, ((K1 if x2 is None else x2.shape[-1]), F))
+    rows_shape = tuple(x.shape[:-1])
+    rows = 1
+    for n in rows_shape:
+        rows *= n
+    ptrs = [_dev(x, "x", bf, rows_shape + (K1,)), _dev(w, "w", bf, (K1, F)), _dev(x2, "x2", bf, rows_shape + (K2,)), _dev(w2, "w2", bf)]
+    return ptrs, ACTIVATIONS[act], (rows, K1, K2, F)
+
+
+def gated_linear(x, w, x2=None, w2=None, act="silu", out=None, stream=None):
+    """gf_gated_linear: act(x @ w) * (x2 @ w2); without w2, act(x @ w); with w2 and without x2, both products are of x.
+    x: [..., K1], x2: [..., K2], w: [K1, F], w2: [K2, F], all bf16 contiguous CUDA tensors; act: "sigmoid", "relu2", "silu" or
+    "gelu".  Returns [..., F] bf16 (allocated here unless passed as out)."""
+    lib = _lib or load_library()
+    ptrs, code, (rows, K1, K2, F) = _gated_args(x, w, x2, w2, act)
+    _one_device(x=x, w=w, x2=x2, w2=w2, out=out)
+    shape = tuple(x.shape[:-1]) + (F,)
+    if out is None:
+        out = torch.empty(shape, device=x.device, dtype=torch.bfloat16)
+    with _on(x):
+        _check(lib.gf_gated_linear(*ptrs, code, _dev(out, "out", torch.bfloat16, shape), rows, K1, K2, F, _stream(stream)), "gf_gated_linear")
+    return out
+
+
+def gated_linear_backward(x, w, dy, x2=None, w2=None, act="silu", stream=None, workspace=None):
+    """gf_gated_linear_backward: gradient of gated_linear(x, w, x2, w2, act).  dy: [..., F] bf16.  Returns (dx, dw, dx2, dw2) in
+    bf16; dx2 is None without x2 (dx then has both products' parts), dw2 without w2.  The workspace, unless a uint8 tensor of
+    enough bytes is passed, is allocated here."""
+    lib = _lib or load_library()
+    ptrs, code, (rows, K1, K2, F) = _gated_args(x, w, x2, w2, act)
+    _one_device(x=x, w=w, x2=x2, w2=w2, dy=dy, workspace=workspace)
+    outs = [None if t is None else torch.empty_like(t) for t in (x, w, x2, w2)]
+    with _on(x):
+        nbytes = int(lib.gf_gated_linear_backward_workspace_bytes(rows, F, w2 is not None))
+        ws = workspace if workspace is not None and workspace.numel() >= nbytes else torch.empty(max(nbytes, 16), dtype=torch.uint8, device=x.device)
+        _check(lib.gf_gated_linear_backward(*ptrs, code, _dev(dy, "dy", torch.bfloat16, tuple(x.shape[:-1]) + (F,)), *(_dev(t, "gradient") for t in outs),
+                                            rows, K1, K2, F, _dev(ws, "workspace"), ws.numel(), _stream(stream)), "gf_gated_linear_backward")
+    return tuple(outs)
+
+
+def _vocab_args(x, w, targets):
+    """Device pointers and sizes of the vocabulary loss's inputs: (pointers, (rows, D, V), shape of the rows)."""
+    V, D = w.shape
+    shape = tuple(x.shape[:-1])
+    rows = 1
+    for n in shape:
+        rows *= n
+    ptrs = [_dev(x, "x", torch.bfloat16, shape + (D,)), _dev(w, "w", torch.bfloat16), _dev(targets, "targets", torch.int64, shape)]
+    return ptrs, (rows, D, V), shape
+
+
+def vocab_loss(x, w, targets, stream=None, workspace=None):
+    """gf_vocab_loss: cross entropy of the logits x @ w.T without keeping them.  x: [..., D] bf16, w: [V, D] bf16, targets: [...]
+    int64 (outside 0..V-1, such as -100: the row has no target and its loss is 0), contiguous CUDA tensors.  Returns (loss, lse),
+    fp32 [...]; lse is what vocab_loss_backward() takes.  The workspace, unless a uint8 tensor of enough bytes is passed, is
+    allocated here."""
+    lib = _lib or load_library()
+    ptrs, (rows, D, V), shape = _vocab_args(x, w, targets)
+    _one_device(x=x, w=w, targets=targets, workspace=workspace)
+    loss, lse = (torch.empty(shape, device=x.device, dtype=torch.float32) for _ in range(2))
+    with _on(x):
+        nbytes = int(lib.gf_vocab_loss_workspace_bytes(rows, V))
+        ws = workspace if workspace is not None and workspace.numel() >= nbytes else torch.empty(max(nbytes, 16), dtype=torch.uint8, device=x.device)
+        _check(lib.gf_vocab_loss(*ptrs, loss.data_ptr(), lse.data_ptr(), rows, D, V, _dev(ws, "workspace"), ws.numel(), _stream(stream)), "gf_vocab_loss")
+    return loss, lse
+
+
+def vocab_loss_backward(x, w, targets, lse, dloss=None, stream=None, workspace=None):
+    """gf_vocab_loss_backward: gradient of sum(dloss * loss) for vocab_loss(x, w, targets), whose lse it takes; dloss: fp32 [...]
+    or None (ones).  Returns (dx, dw) in bf16.  The workspace, unless a uint8 tensor of enough bytes is passed, is allocated here."""
+    lib = _lib or load_library()
+    ptrs, (rows, D, V), shape = _vocab_args(x, w, targets)
+    _one_device(x=x, w=w, targets=targets, lse=lse, dloss=dloss, workspace=workspace)
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    f32 = torch.float32
+    with _on(x):
+        nbytes = int(lib.gf_vocab_loss_backward_workspace_bytes(rows, D, V))
+        ws = workspace if workspace is not None and workspace.numel() >= nbytes else torch.empty(max(nbytes, 16), dtype=torch.uint8, device=x.device)
+        _check(lib.gf_vocab_loss_backward(*ptrs, _dev(lse, "lse", f32, shape), _dev(dloss, "dloss", f32, shape), dx.data_ptr(), dw.data_ptr(), rows, D, V,
+                                          _dev(ws, "workspace"), ws.numel(), _stream(stream)), "gf_vocab_loss_backward")
+    return dx, dw
 
 
 def decay_logit(x, mu_x, A_d, B_d, lambda_d, A_w, B_w, lambda_w, x_prev=None, out=None, stream=None):

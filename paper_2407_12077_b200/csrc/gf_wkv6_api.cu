@@ -8,8 +8,11 @@
 #include <cuda_runtime.h>
 
 #include "decay_logit.cuh"
+#include "gated_linear.cuh"
 #include "key_compress.cuh"
 #include "ln_heads.cuh"
+#include "ln_heads_grad.cuh"
+#include "vocab_loss.cuh"
 #include "wkv6_backward.cuh"
 #include "wkv6_backward_chunked.cuh"
 #include "wkv6_chunked.cuh"
@@ -166,6 +169,56 @@ gf_status_t layernorm_call(const IO* y, const float* gamma, const float* beta, f
     if (!y || !out || misaligned(y) || misaligned(out) || misaligned(gamma) || misaligned(beta)) return GF_ERR_INVALID_ARG;
     return gf::layernorm_heads<IO>(y, gamma, beta, eps, out, rows, (int)D, gf::sm_count(), (cudaStream_t)stream, &g_launches);
 }
+
+template <typename IO>
+gf_status_t layernorm_backward_call(const IO* y, const float* gamma, float eps, const IO* dout, IO* dy, float* dgamma, float* dbeta,
+                                    long long rows, int H, int N, void* workspace, size_t workspace_bytes, gf_stream_t stream)
+{
+    if (rows < 0 || H < 0 || N < 0 || !(eps >= 0.f) || eps > 3.0e38f) return GF_ERR_INVALID_ARG;
+    const long long D = (long long)H * N;
+    const cudaStream_t st = (cudaStream_t)stream;
+    if (D == 0) return GF_OK;
+    if ((D & 7) || D > gf::ln::MAX_D) return GF_ERR_UNSUPPORTED;
+    if (misaligned(dgamma) || misaligned(dbeta)) return GF_ERR_INVALID_ARG;
+    if (rows == 0) {                                 // sums over nothing
+        if (dgamma && cudaMemsetAsync(dgamma, 0, (size_t)D * 4, st) != cudaSuccess) return GF_ERR_CUDA;
+        if (dbeta && cudaMemsetAsync(dbeta, 0, (size_t)D * 4, st) != cudaSuccess) return GF_ERR_CUDA;
+        return GF_OK;
+    }
+    if (rows > (1LL << 62) / D) return GF_ERR_INVALID_ARG;
+    if (!y || !dout || !dy || misaligned(y) || misaligned(dout) || misaligned(dy) || misaligned(gamma) || misaligned(workspace)) return GF_ERR_INVALID_ARG;
+    const int n_sm = gf::sm_count();
+    if (n_sm <= 0) return GF_ERR_CUDA;
+    if ((dgamma || dbeta) && (!workspace || workspace_bytes < gf::layernorm_heads_grad_bytes((int)D, n_sm))) return GF_ERR_WORKSPACE;
+    return gf::layernorm_heads_grad<IO>(y, dout, gamma, eps, dy, dgamma, dbeta, rows, (int)D, static_cast<float*>(workspace), n_sm, st, &g_launches);
+}
+
+// Sizes and operands of the gated linear block; *s is filled in.  GF_OK with s->rows == 0 or s->F == 0: there is nothing to compute.
+gf_status_t check_gated(const void* x, const void* w, const void* x2, const void* w2, int act, long long rows, int K1, int K2, int F, gf::gl::Shape* s)
+{
+    if (rows < 0 || K1 < 0 || K2 < 0 || F < 0 || act < 0 || act > gf::pg::ACT_GELU) return GF_ERR_INVALID_ARG;
+    *s = gf::gl::Shape{rows, K1, w2 ? K2 : 0, F, w2 && !x2};
+    if (rows == 0 || F == 0) return GF_OK;           // (an empty tensor's pointer may be NULL and says nothing)
+    if (w2 ? (!x2 && K2 != K1) : (x2 || K2 != 0)) return GF_ERR_INVALID_ARG;
+    if (K1 == 0 || (w2 && K2 == 0) || (K1 & 7) || (K2 & 7) || (F & 7)) return GF_ERR_UNSUPPORTED;
+    const long long widest = K1 > F ? (K1 > K2 ? K1 : K2) : (F > K2 ? F : K2);
+    if (rows >= (1LL << 31) - 256 || widest >= (1LL << 31) - 256 || (rows / 64 + 1) * (widest / 64 + 1) >= 1LL << 30) return GF_ERR_UNSUPPORTED;
+    if ((long long)(K1 / 64 + 1) * (F / 64 + 1) >= 1LL << 29 || (long long)(K2 / 64 + 1) * (F / 64 + 1) >= 1LL << 29) return GF_ERR_UNSUPPORTED;
+    if (!x || !w || misaligned(x) || misaligned(w) || misaligned(x2) || misaligned(w2)) return GF_ERR_INVALID_ARG;
+    return GF_OK;
+}
+
+gf_status_t check_vocab(const void* x, const void* w, const void* targets, long long rows, int D, long long V)
+{
+    if (rows < 0 || D < 0 || V <= 0) return GF_ERR_INVALID_ARG;
+    if (rows == 0) return GF_OK;
+    if (D == 0 || (D & 7)) return GF_ERR_UNSUPPORTED;
+    if (rows >= (1LL << 31) - 256 || V >= (1LL << 31) - 256 || (rows / 128 + 1) * (V / 128 + 1) >= 1LL << 30) return GF_ERR_UNSUPPORTED;
+    if ((rows / 128 + V / 128 + 2) * (D / 128 + 1) >= 1LL << 30) return GF_ERR_UNSUPPORTED;
+    if (!x || !w || !targets || misaligned(x) || misaligned(w) || misaligned(targets)) return GF_ERR_INVALID_ARG;
+    return GF_OK;
+}
+gf_status_t zeros(void* p, size_t bytes, cudaStream_t st) { return cudaMemsetAsync(p, 0, bytes, st) == cudaSuccess ? GF_OK : GF_ERR_CUDA; }
 }  // namespace
 
 extern "C" {
@@ -818,6 +871,110 @@ gf_status_t gf_c2_decay_logit(const void* x, const void* x_prev, const float* mu
         if (misaligned(q)) return GF_ERR_INVALID_ARG;
     return gf::decay_logit((const bf*)x, (const bf*)x_prev, mu_x, (const bf*)A_d, (const bf*)B_d, lambda_d, (const bf*)A_w,
                            (const bf*)B_w, lambda_w, (bf*)d, B, T, D, Rd, Rw, (cudaStream_t)stream, &g_launches);
+}
+
+gf_status_t gf_c2_layernorm_backward(const void* y, const float* gamma, float eps, const void* dout, void* dy, float* dgamma, float* dbeta,
+                                     long long rows, int H, int N, void* workspace, size_t workspace_bytes, gf_stream_t stream)
+{
+    using bf = __nv_bfloat16;
+    return layernorm_backward_call(static_cast<const bf*>(y), gamma, eps, static_cast<const bf*>(dout), static_cast<bf*>(dy), dgamma, dbeta, rows, H, N,
+                                   workspace, workspace_bytes, stream);
+}
+
+gf_status_t gf_c2_layernorm_backward_f32(const float* y, const float* gamma, float eps, const float* dout, float* dy, float* dgamma, float* dbeta,
+                                         long long rows, int H, int N, void* workspace, size_t workspace_bytes, gf_stream_t stream)
+{
+    return layernorm_backward_call(y, gamma, eps, dout, dy, dgamma, dbeta, rows, H, N, workspace, workspace_bytes, stream);
+}
+
+size_t gf_c2_layernorm_backward_workspace_bytes(int H, int N)
+{
+    const long long D = (long long)H * N;
+    const int n_sm = gf::sm_count();
+    if (H <= 0 || N <= 0 || (D & 7) || D > gf::ln::MAX_D || n_sm <= 0) return 0;
+    return gf::layernorm_heads_grad_bytes((int)D, n_sm);
+}
+
+gf_status_t gf_gated_linear(const void* x, const void* w, const void* x2, const void* w2, int act, void* y, long long rows, int K1, int K2, int F,
+                            gf_stream_t stream)
+{
+    using bf = __nv_bfloat16;
+    gf::gl::Shape s;
+    const gf_status_t e = check_gated(x, w, x2, w2, act, rows, K1, K2, F, &s);
+    if (e != GF_OK || rows == 0 || F == 0) return e;
+    if (!y || misaligned(y) || y == x || y == w || y == x2 || y == w2) return GF_ERR_INVALID_ARG;
+    if (w2 && x2 == x && K1 == K2) s.same = true;
+    return gf::gated_linear((const bf*)x, (const bf*)w, (const bf*)(x2 ? x2 : x), (const bf*)w2, act, (bf*)y, s, (cudaStream_t)stream, &g_launches);
+}
+
+gf_status_t gf_gated_linear_backward(const void* x, const void* w, const void* x2, const void* w2, int act, const void* dy, void* dx, void* dw,
+                                     void* dx2, void* dw2, long long rows, int K1, int K2, int F, void* workspace, size_t workspace_bytes,
+                                     gf_stream_t stream)
+{
+    using bf = __nv_bfloat16;
+    const cudaStream_t st = (cudaStream_t)stream;
+    gf::gl::Shape s;
+    const gf_status_t e = check_gated(x, w, x2, w2, act, rows, K1, K2, F, &s);
+    if (e != GF_OK) return e;
+    if (rows == 0 || F == 0) {                       // sums over nothing
+        if (dx && zeros(dx, (size_t)rows * K1 * 2, st) != GF_OK) return GF_ERR_CUDA;
+        if (dx2 && zeros(dx2, (size_t)rows * K2 * 2, st) != GF_OK) return GF_ERR_CUDA;
+        if (dw && zeros(dw, (size_t)K1 * F * 2, st) != GF_OK) return GF_ERR_CUDA;
+        if (dw2 && zeros(dw2, (size_t)K2 * F * 2, st) != GF_OK) return GF_ERR_CUDA;
+        return GF_OK;
+    }
+    if (!dy || !dx || !dw || (w2 != nullptr) != (dw2 != nullptr) || (x2 != nullptr) != (dx2 != nullptr)) return GF_ERR_INVALID_ARG;
+    const void* outs[] = {dx, dw, dx2, dw2};
+    const void* ins[] = {x, w, x2, w2, dy};
+    if (misaligned(dy) || misaligned(workspace)) return GF_ERR_INVALID_ARG;
+    for (int i = 0; i < 4; ++i) {
+        if (!outs[i]) continue;
+        if (misaligned(outs[i])) return GF_ERR_INVALID_ARG;
+        for (const void* q : ins)
+            if (outs[i] == q) return GF_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (outs[i] == outs[j]) return GF_ERR_INVALID_ARG;
+    }
+    if (!workspace || workspace_bytes < gf::gated_linear_backward_bytes(rows, F, w2 != nullptr)) return GF_ERR_WORKSPACE;
+    return gf::gated_linear_backward((const bf*)x, (const bf*)w, (const bf*)(x2 ? x2 : x), (const bf*)w2, act, (const bf*)dy, (bf*)dx, (bf*)dw, (bf*)dx2,
+                                     (bf*)dw2, s, static_cast<bf*>(workspace), st, &g_launches);
+}
+
+size_t gf_gated_linear_backward_workspace_bytes(long long rows, int F, int gated)
+{
+    return rows <= 0 || F <= 0 ? 0 : gf::gated_linear_backward_bytes(rows, F, gated != 0);
+}
+
+gf_status_t gf_vocab_loss(const void* x, const void* w, const int64_t* targets, float* loss, float* lse, long long rows, int D, long long V,
+                          void* workspace, size_t workspace_bytes, gf_stream_t stream)
+{
+    using bf = __nv_bfloat16;
+    const gf_status_t e = check_vocab(x, w, targets, rows, D, V);
+    if (e != GF_OK || rows == 0) return e;
+    if (!loss || !lse || loss == lse || misaligned(loss) || misaligned(lse) || misaligned(workspace)) return GF_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < gf::vocab_loss_bytes(rows, V)) return GF_ERR_WORKSPACE;
+    return gf::vocab_loss((const bf*)x, (const bf*)w, (const long long*)targets, loss, lse, rows, D, V, workspace, (cudaStream_t)stream, &g_launches);
+}
+
+gf_status_t gf_vocab_loss_backward(const void* x, const void* w, const int64_t* targets, const float* lse, const float* dloss, void* dx, void* dw,
+                                   long long rows, int D, long long V, void* workspace, size_t workspace_bytes, gf_stream_t stream)
+{
+    using bf = __nv_bfloat16;
+    const gf_status_t e = check_vocab(x, w, targets, rows, D, V);
+    if (e != GF_OK) return e;
+    if (rows == 0) return dw && D > 0 ? zeros(dw, (size_t)V * D * 2, (cudaStream_t)stream) : GF_OK;
+    if (!lse || !dx || !dw || dx == dw || dx == x || dx == w || dw == x || dw == w) return GF_ERR_INVALID_ARG;
+    if (misaligned(lse) || misaligned(dloss) || misaligned(dx) || misaligned(dw) || misaligned(workspace)) return GF_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < gf::vocab_loss_backward_bytes(rows, D, V)) return GF_ERR_WORKSPACE;
+    return gf::vocab_loss_backward((const bf*)x, (const bf*)w, (const long long*)targets, lse, dloss, (bf*)dx, (bf*)dw, rows, D, V, workspace,
+                                   (cudaStream_t)stream, &g_launches);
+}
+
+size_t gf_vocab_loss_workspace_bytes(long long rows, long long V) { return rows <= 0 || V <= 0 ? 0 : gf::vocab_loss_bytes(rows, V); }
+
+size_t gf_vocab_loss_backward_workspace_bytes(long long rows, int D, long long V)
+{
+    return rows <= 0 || D <= 0 || V <= 0 ? 0 : gf::vocab_loss_backward_bytes(rows, D, V);
 }
 
 const char* gf_status_string(gf_status_t s)

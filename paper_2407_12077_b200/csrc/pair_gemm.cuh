@@ -1,0 +1,630 @@
+// Matrix products with the elementwise work of an operator in their epilogue, for sm_100a (tcgen05 + TMEM + TMA): what the
+// gated linear block and the vocabulary loss, and the gradients of both, are built from.
+//
+//     C[m][n] = sum_k A(m, k) B(k, n)        bf16 operands, fp32 accumulators
+//
+// Either operand may lie with its contraction index or its other index contiguous in memory (K-major, MN-major); both are read by
+// TMA as they are, in 64 x 64 tiles, so a gradient's products (dy W^T, x^T dy) need no transposed copies.  A launch computes one
+// or more groups of output tiles (two gradients of one call), whose tiles are handed out in order to persistent units: a unit
+// is a pair of CTAs on neighbouring SMs that works on 256 x 256 accumulators with cta_group::2 instructions (each CTA holds 128 rows
+// of A and of the result, and half the columns of B; one instruction of the leading CTA feeds both tensor cores, and every byte of
+// an operand enters shared memory once), or, where a call has too few such tiles to fill the GPU, one CTA with 128 x 128 ones.
+// Two accumulator sets fill tensor memory: the products of a tile run while the epilogue drains the one before.
+//
+// A tile's columns can be shared out in halves (B_DUAL, B_HALF): the left half holds columns of a first product, the right half the
+// same columns of a second one, so that an epilogue sees both values of an element (the gated linear block).  B_DUAL: both
+// products have the same A and run as one; B_HALF: each has its own A and depth, and they run one after the other.
+//
+//   warp 0      TMA producer: 64 contraction indices of A and B (16 KB each per CTA) per stage of a six-stage ring
+//   warp 1      tensor-memory allocation; an elected lane of the leading CTA issues the four products of a stage
+//   warps 2-5   epilogue: a lane owns a row of the tile, 32 columns at a time
+// Every wait is bounded (status flag and abort as in the prefill kernel); a pair's CTAs meet before either leaves.
+#pragma once
+#include "key_compress.cuh"
+#include "wkv6_chunked.cuh"
+
+namespace gf {
+namespace pg {
+
+using namespace ck;                                   // PTX wrappers, descriptors, TILE, bounded waits
+using kc::cluster_sync;
+using kc::tmem_ld_row32;
+
+constexpr int THREADS = 192;
+constexpr int NSTAGE = 6;
+constexpr int STAGE_BYTES = 4 * TILE;                 // 128 x 64 of A, 128 x 64 of B
+constexpr int OFF_SLAB = NSTAGE * STAGE_BYTES;        // [4 warps][2][32 rows x 128 B]
+constexpr int OFF_MISC = OFF_SLAB + 4 * 2 * 4096;     // abort word, wait limit, tensor-memory address, barriers
+constexpr int SMEM = OFF_MISC + 256 + 1024;           // + slack for manual 1024-byte alignment
+static_assert(SMEM <= 232448, "shared memory budget of one sm_100 CTA");
+enum { BAR_FULL = 0, BAR_EMPTY = NSTAGE, BAR_ACC_FULL = 2 * NSTAGE, BAR_ACC_EMPTY = BAR_ACC_FULL + 2, BAR_DRAIN = BAR_ACC_EMPTY + 2, N_BARS };
+static_assert(16 + 8 * N_BARS <= 256, "barrier block");
+
+// what the epilogue makes of an accumulator
+enum Epilogue {
+    EPI_STORE,          // the product itself (Group::mode)
+    EPI_GATE,           // act(a) * b of the two halves, or act(a) of a whole tile
+    EPI_GATE_GRAD,      // dy b act'(a) and dy act(a)
+    EPI_LSE,            // per row and tile of columns: maximum and sum of exponentials, and the target's logit
+    EPI_PROB            // (exp(z - lse) - [column is the target]) * dloss
+};
+enum BCols : unsigned char { B_WHOLE, B_DUAL, B_HALF };
+enum OutMode : unsigned char { OUT_BF16, OUT_F32, OUT_F32_ADD, OUT_BF16_ADD };   // (_ADD: onto, resp. with, the fp32 sums of earlier launches)
+enum Act { ACT_SIGMOID = 0, ACT_RELU2 = 1, ACT_SILU = 2, ACT_GELU = 3 };
+
+// A run of contraction indices of a group's products: 64 * steps of them (the last may reach past the tensors, where TMA reads zeros).
+struct Segment {
+    unsigned char a, b;             // tensor maps (B_DUAL: b and b + 1)
+    bool a_mn, b_mn;                // the operand's non-contraction index is the contiguous one
+    BCols cols;
+    bool right;                     // B_HALF: accumulates in the tile's right half
+    bool fresh;                     // the first products into these accumulators
+    int steps;
+};
+struct Group {
+    int tiles_m, tiles_n, first;    // first: number of the group's first tile in the launch
+    int n_seg;
+    Segment seg[2];
+    unsigned char out;              // tensor map of the result
+    OutMode mode;
+    int rows, cols;                 // extent of the result (of each half's columns where a tile is halved)
+    float* part;                    // OUT_BF16_ADD: fp32 sums [rows][cols]
+};
+constexpr int MAX_IN = 8, MAX_OUT = 4, MAX_GROUPS = 4;
+struct GemmParams {
+    CUtensorMap in[MAX_IN], out[MAX_OUT];
+    Group g[MAX_GROUPS];
+    int n_groups, n_tiles;
+    // EPI_GATE, EPI_GATE_GRAD
+    int act;
+    bool gated;
+    const __nv_bfloat16* dy;
+    // EPI_LSE, EPI_PROB
+    const long long* targets;
+    long long vocab;                // a target outside [0, vocab) is none
+    int first_col;                  // the vocabulary's index of this launch's first column
+    float2* stats;                  // [tiles_n][rows] (reference value, sum of exponentials over it)
+    float* target_logit;
+    const float* lse;
+    const float* dloss;             // or nullptr: ones
+};
+
+// ---------------------------------------------------------------- PTX of CTA pairs
+__device__ __forceinline__ uint32_t map_to_leader(uint32_t saddr)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(saddr));
+    return a;
+}
+__device__ __forceinline__ void arrive_cluster_if(uint32_t addr, bool pred)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\t@p mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n\t}"
+                 ::"r"(addr), "r"((uint32_t)pred) : "memory");
+}
+// A tile into this CTA's shared memory; its bytes are counted by the barrier at a shared::cluster address, the leading CTA's.
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* tm, int c0, int c1, uint32_t bar_cluster)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(dst), "l"(tm), "r"(c0), "r"(c1), "r"(bar_cluster) : "memory");
+}
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t smem_dst, uint32_t cols)      // one full warp of either CTA
+{
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t cols)
+{
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void tc_mma_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// One arrival at the barrier of both CTAs of the pair once the products issued so far are complete.
+__device__ __forceinline__ void tc_commit_pair(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"((unsigned short)3) : "memory");
+}
+__device__ __forceinline__ void tma_reduce_add_2d(const CUtensorMap* tm, int c0, int c1, uint32_t src)
+{
+    asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];"
+                 ::"l"(tm), "r"(c0), "r"(c1), "r"(src) : "memory");
+}
+
+// K-major: 8-row groups 1024 bytes apart.  MN-major: blocks of 64 indices a tile apart.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t saddr, bool mn) { return mn ? kc::kc_desc_w(saddr) : smem_desc(saddr); }
+// fp32 accumulator, bf16 A and B
+__device__ __forceinline__ uint32_t instr_desc(int m, int n, bool a_mn, bool b_mn)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+// ---------------------------------------------------------------- activations
+// 1 / (1 + exp(-|a|)) and exp(-|a|): both sides of the sigmoid from an exponential that cannot overflow
+__device__ __forceinline__ float act_value(int act, float a)
+{
+    if (act == ACT_RELU2) {
+        const float r = fmaxf(a, 0.f);
+        return a != a ? a : r * r;
+    }
+    if (act == ACT_GELU) return a * (0.5f * erfcf(a * -0.70710678f));
+    const float s = __fdividef(1.f, 1.f + __expf(-a));
+    return act == ACT_SIGMOID ? s : a * s;
+}
+// value and derivative
+__device__ __forceinline__ void act_grad(int act, float a, float& f, float& df)
+{
+    if (act == ACT_RELU2) {
+        const float r = a != a ? a : fmaxf(a, 0.f);
+        f = r * r;
+        df = 2.f * r;
+    } else if (act == ACT_GELU) {
+        const float phi = 0.5f * erfcf(a * -0.70710678f);
+        f = a * phi;
+        df = fmaf(a * 0.39894228f, __expf(-0.5f * a * a), phi);
+    } else {
+        const float e = __expf(-fabsf(a)), r = __fdividef(1.f, 1.f + e);
+        const float s = a >= 0.f ? r : e * r, t = a >= 0.f ? e * r : r;      // t = 1 - s without cancellation
+        f = act == ACT_SIGMOID ? s : a * s;
+        df = act == ACT_SIGMOID ? s * t : s * fmaf(a, t, 1.f);
+    }
+}
+
+__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
+{
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+// 32 values of the lane's row, rounded to bf16, into columns 32*half .. of a 64-column slab
+__device__ __forceinline__ void put_bf16(uint32_t slab, int lane, int half, const float (&o)[32])
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        sts128(slab + swz(lane, (4 * half + q) << 4), pack_bf16(o[8 * q], o[8 * q + 1]), pack_bf16(o[8 * q + 2], o[8 * q + 3]),
+               pack_bf16(o[8 * q + 4], o[8 * q + 5]), pack_bf16(o[8 * q + 6], o[8 * q + 7]));
+}
+__device__ __forceinline__ void ld_acc(uint32_t taddr, float (&o)[32])
+{
+    uint32_t v[32];
+    tmem_ld_row32(taddr, v);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) o[j] = __uint_as_float(v[j]);
+}
+
+__device__ __forceinline__ void tile_at(const GemmParams& p, int tile, int& gi, int& tm, int& tn)
+{
+    gi = 0;
+    while (gi + 1 < p.n_groups && tile >= p.g[gi + 1].first) ++gi;
+    const Group& g = p.g[gi];
+    // bands of eight tiles along m, column by column: the tiles that run at one time share few rows of A and of B
+    const int i = tile - g.first, per = 8 * g.tiles_n, band = i / per, rest = i - band * per;
+    const int h = min(8, g.tiles_m - 8 * band);
+    tn = rest / h;
+    tm = 8 * band + rest - tn * h;
+}
+
+template <int CG, Epilogue EPI>
+__global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_constant__ GemmParams p)
+{
+    constexpr int BN = 128 * CG;                      // columns of a tile
+    constexpr int HW = BN / 2;
+    constexpr int ACC_COLS = 256;                     // two accumulator sets
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const uint32_t sbase = smem_u32(smem);
+    const uint32_t abort_flag = sbase + OFF_MISC;
+    auto bar = [&](int i) { return sbase + OFF_MISC + 16 + 8 * i; };
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    uint32_t rank = 0;
+    if constexpr (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const int unit = blockIdx.x / CG, units = gridDim.x / CG;
+
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (tid == 0) {
+        for (int i = 0; i < NSTAGE; ++i) {
+            mbar_init(bar(BAR_FULL + i), 1);
+            mbar_init(bar(BAR_EMPTY + i), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(BAR_ACC_FULL + i), 1);
+            mbar_init(bar(BAR_ACC_EMPTY + i), 4 * CG);
+        }
+        mbar_init(bar(BAR_DRAIN), 1);
+        sts32(abort_flag, 0u);
+        sts32(abort_flag + 4, ck::WAIT_LIMIT_US);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async();
+    }
+    if (warp == 1) {
+        if constexpr (CG == 2) tmem_alloc_pair(sbase + OFF_MISC + 8, 512);
+        else tmem_alloc(sbase + OFF_MISC + 8, 512);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync();            // the other CTA's barriers are there before anything arrives at them
+    tc_fence_after();
+    const uint32_t tmem = lds32(sbase + OFF_MISC + 8);
+
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (warp == 0) {
+        // ============================== TMA producer ==============================
+        int s = 0, ph = 0, issued = 0;
+        bool alive = true;
+        for (int tile = unit; tile < p.n_tiles && alive; tile += units) {
+            int gi, tm, tn;
+            tile_at(p, tile, gi, tm, tn);
+            const Group& g = p.g[gi];
+            const int m0 = tm * 128 * CG + 128 * (int)rank;
+            for (int q = 0; q < g.n_seg && alive; ++q) {
+                const Segment sg = g.seg[q];
+                // this CTA's columns of B: 128 of the tile's (one block of 64 where the tile's halves have products of their own)
+                const int n0 = sg.cols == B_WHOLE ? tn * BN + 128 * (int)rank : sg.cols == B_DUAL ? tn * HW : tn * HW + 64 * (int)rank;
+                const int n1 = sg.cols == B_DUAL && CG == 1 ? n0 : n0 + 64;
+                const CUtensorMap* ma = &p.in[sg.a];
+                const CUtensorMap* mb0 = &p.in[sg.b + (sg.cols == B_DUAL && CG == 2 ? rank : 0)];
+                const CUtensorMap* mb1 = sg.cols == B_DUAL && CG == 1 ? &p.in[sg.b + 1] : mb0;
+                for (int ks = 0; ks < sg.steps; ++ks) {
+                    if (issued >= NSTAGE && !mbar_wait_warp(bar(BAR_EMPTY + s), ph ^ 1, abort_flag)) { alive = false; break; }
+                    const uint32_t st = sbase + s * STAGE_BYTES;
+                    if (elect_one()) {
+                        const int k = ks * 64;
+                        const uint32_t full = CG == 2 ? map_to_leader(bar(BAR_FULL + s)) : bar(BAR_FULL + s);
+                        auto load = [&](uint32_t dst, const CUtensorMap* m, int c0, int c1) {
+                            if constexpr (CG == 2) tma_load_pair(dst, m, c0, c1, full);
+                            else tma_load_2d(dst, m, c0, c1, full);
+                        };
+                        if (rank == 0) mbar_expect_tx(bar(BAR_FULL + s), (sg.cols == B_HALF ? 3 : 4) * TILE * CG);
+                        load(st, ma, sg.a_mn ? m0 : k, sg.a_mn ? k : m0);
+                        load(st + TILE, ma, sg.a_mn ? m0 + 64 : k, sg.a_mn ? k : m0 + 64);
+                        load(st + 2 * TILE, mb0, sg.b_mn ? n0 : k, sg.b_mn ? k : n0);
+                        if (sg.cols != B_HALF) load(st + 3 * TILE, mb1, sg.b_mn ? n1 : k, sg.b_mn ? k : n1);
+                    }
+                    __syncwarp();
+                    ++issued;
+                    if (++s == NSTAGE) { s = 0; ph ^= 1; }
+                }
+            }
+        }
+        // do not leave while copies may still be in flight (a pair's are counted by the leading CTA, and its CTAs leave together)
+        if (rank == 0) {
+            for (int c = min(issued, NSTAGE); c > 0; --c) {
+                // stages s - c .. s - 1, each in the phase of its last use
+                const int st = s - c < 0 ? s - c + NSTAGE : s - c, sp = s - c < 0 ? ph ^ 1 : ph;
+                if (!mbar_wait_warp(bar(BAR_FULL + st), sp, abort_flag, false)) break;
+            }
+        }
+    } else if (warp == 1) {
+        // ============================== MMA issuer (leading CTA) ==============================
+        if (rank == 0) {
+            int s = 0, ph = 0, ti = 0;
+            bool alive = true;
+            for (int tile = unit; tile < p.n_tiles && alive; tile += units, ++ti) {
+                int gi, tm, tn;
+                tile_at(p, tile, gi, tm, tn);
+                const Group& g = p.g[gi];
+                const int set = ti & 1, use = ti >> 1;
+                // the epilogue has read this set's previous tile out of tensor memory
+                if (use >= 1 && !mbar_wait_warp(bar(BAR_ACC_EMPTY + set), (use + 1) & 1, abort_flag)) { alive = false; break; }
+                tc_fence_after();
+                for (int q = 0; q < g.n_seg && alive; ++q) {
+                    const Segment sg = g.seg[q];
+                    const uint32_t idesc = instr_desc(128 * CG, sg.cols == B_HALF ? HW : BN, sg.a_mn, sg.b_mn);
+                    const uint32_t acc = tmem + ACC_COLS * set + (sg.right ? HW : 0);
+                    const uint64_t a_step = sg.a_mn ? 128 : 2, b_step = sg.b_mn ? 128 : 2;      // 16 contraction indices
+                    for (int ks = 0; ks < sg.steps; ++ks) {
+                        if (!mbar_wait_warp(bar(BAR_FULL + s), ph, abort_flag)) { alive = false; break; }
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint32_t st = sbase + s * STAGE_BYTES;
+                            const uint64_t da = operand_desc(st, sg.a_mn), db = operand_desc(st + 2 * TILE, sg.b_mn);
+#pragma unroll
+                            for (int kk = 0; kk < 4; ++kk) {
+                                const uint32_t on = !sg.fresh || ks > 0 || kk > 0;
+                                if constexpr (CG == 2) tc_mma_pair(acc, da + a_step * kk, db + b_step * kk, idesc, on);
+                                else tc_mma(acc, da + a_step * kk, db + b_step * kk, idesc, on);
+                            }
+                            const bool last = ks == sg.steps - 1 && q == g.n_seg - 1;
+                            if constexpr (CG == 2) {
+                                tc_commit_pair(bar(BAR_EMPTY + s));
+                                if (last) tc_commit_pair(bar(BAR_ACC_FULL + set));
+                            } else {
+                                tc_commit(bar(BAR_EMPTY + s));
+                                if (last) tc_commit(bar(BAR_ACC_FULL + set));
+                            }
+                        }
+                        __syncwarp();
+                        if (++s == NSTAGE) { s = 0; ph ^= 1; }
+                    }
+                }
+            }
+            if (!alive) {                             // products in flight end before tensor memory is given back
+                if (elect_one()) {
+                    if constexpr (CG == 2) tc_commit_pair(bar(BAR_DRAIN));
+                    else tc_commit(bar(BAR_DRAIN));
+                }
+                __syncwarp();
+                mbar_wait_warp(bar(BAR_DRAIN), 0, abort_flag, false);
+            }
+        }
+    } else {
+        // ============================== epilogue warps ==============================
+        const int sp = warp & 3;                      // tensor-memory sub-partition: accumulator rows 32*sp .. 32*sp+31
+        const uint32_t slabs = sbase + OFF_SLAB + (warp - 2) * 2 * 4096;
+        int ti = 0, sb = 0;
+        for (int tile = unit; tile < p.n_tiles; tile += units, ++ti) {
+            int gi, tm, tn;
+            tile_at(p, tile, gi, tm, tn);
+            const Group& g = p.g[gi];
+            const int set = ti & 1;
+            if (!mbar_wait_warp(bar(BAR_ACC_FULL + set), (ti >> 1) & 1, abort_flag)) break;
+            tc_fence_after();
+            const uint32_t acc = tmem + ((uint32_t)(32 * sp) << 16) + ACC_COLS * set;
+            const int row0 = tm * 128 * CG + 128 * (int)rank + 32 * sp, row = row0 + lane;
+            const bool in = row < g.rows;
+            // a slab that no store is reading any more
+            auto take_slab = [&]() {
+                if (lane == 0) bulk_wait_read<1>();
+                __syncwarp();
+                const uint32_t sl = slabs + 4096 * sb;
+                sb ^= 1;
+                return sl;
+            };
+            auto send = [&](const CUtensorMap* m, int col, uint32_t sl) {
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) {                      // (a group each time, if an empty one: take_slab() counts them)
+                    if (row0 < g.rows) tma_store_2d(m, col, row0, sl);
+                    bulk_commit();
+                }
+            };
+            if constexpr (EPI == EPI_STORE) {
+                if (g.mode == OUT_F32 || g.mode == OUT_F32_ADD) {
+                    for (int c = 0; c < BN; c += 32) {
+                        const int col = tn * BN + c;
+                        if (col >= g.cols) break;
+                        float v[32];
+                        ld_acc(acc + c, v);
+                        const uint32_t sl = take_slab();
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            sts128(sl + swz(lane, q << 4), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
+                        fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (row0 < g.rows) {
+                                if (g.mode == OUT_F32) tma_store_2d(&p.out[g.out], col, row0, sl);
+                                else tma_reduce_add_2d(&p.out[g.out], col, row0, sl);
+                            }
+                            bulk_commit();
+                        }
+                    }
+                } else {
+                    for (int c = 0; c < BN; c += 64) {
+                        const int col = tn * BN + c;
+                        if (col >= g.cols) break;
+                        const uint32_t sl = take_slab();
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            float v[32];
+                            ld_acc(acc + c + 32 * half, v);
+                            if (g.mode == OUT_BF16_ADD && in) {
+                                const float* src = g.part + (size_t)row * g.cols + col + 32 * half;
+#pragma unroll
+                                for (int q = 0; q < 8; ++q)
+                                    if (col + 32 * half + 4 * q < g.cols) {          // (a multiple of 8)
+                                        const float4 f = __ldcs(reinterpret_cast<const float4*>(src) + q);
+                                        v[4 * q] += f.x; v[4 * q + 1] += f.y; v[4 * q + 2] += f.z; v[4 * q + 3] += f.w;
+                                    }
+                            }
+                            put_bf16(sl, lane, half, v);
+                        }
+                        send(&p.out[g.out], col, sl);
+                    }
+                }
+            } else if constexpr (EPI == EPI_GATE) {
+                const int width = p.gated ? HW : BN;
+                for (int c = 0; c < width; c += 64) {
+                    const int col = tn * width + c;
+                    if (col >= g.cols) break;
+                    const uint32_t sl = take_slab();
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        float a[32];
+                        ld_acc(acc + c + 32 * half, a);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) a[j] = act_value(p.act, a[j]);
+                        if (p.gated) {
+                            float b[32];
+                            ld_acc(acc + HW + c + 32 * half, b);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) a[j] *= b[j];
+                        }
+                        put_bf16(sl, lane, half, a);
+                    }
+                    send(&p.out[0], col, sl);
+                }
+            } else if constexpr (EPI == EPI_GATE_GRAD) {
+                const int width = p.gated ? HW : BN;
+                for (int c = 0; c < width; c += 64) {
+                    const int col = tn * width + c;
+                    if (col >= g.cols) break;
+                    if (lane == 0) bulk_wait_read<0>();
+                    __syncwarp();
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        uint32_t d[16];
+                        const __nv_bfloat16* src = p.dy + (size_t)row * g.cols + col + 32 * half;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const uint4 u = in && col + 32 * half + 8 * q < g.cols ? __ldg(reinterpret_cast<const uint4*>(src) + q) : make_uint4(0u, 0u, 0u, 0u);
+                            d[4 * q] = u.x; d[4 * q + 1] = u.y; d[4 * q + 2] = u.z; d[4 * q + 3] = u.w;
+                        }
+                        float a[32], b[32];
+                        ld_acc(acc + c + 32 * half, a);
+                        if (p.gated) ld_acc(acc + HW + c + 32 * half, b);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float dy = __uint_as_float(j & 1 ? d[j / 2] & 0xffff0000u : d[j / 2] << 16);
+                            float f, df;
+                            act_grad(p.act, a[j], f, df);
+                            a[j] = p.gated ? dy * b[j] * df : dy * df;
+                            b[j] = dy * f;
+                        }
+                        put_bf16(slabs, lane, half, a);
+                        if (p.gated) put_bf16(slabs + 4096, lane, half, b);
+                    }
+                    send(&p.out[0], col, slabs);
+                    if (p.gated) send(&p.out[1], col, slabs + 4096);
+                }
+            } else if constexpr (EPI == EPI_LSE) {
+                // exp is taken of differences to a reference, the largest value so far (0 instead of an infinite one: the sum is then
+                // infinite, or zero, by itself); a NaN reaches the sum through its own exponential
+                float ref = -INFINITY, sum = 0.f;
+                const long long t = in ? p.targets[row] : -1;
+                for (int c = 0; c < BN; c += 32) {
+                    const int col = tn * BN + c;
+                    if (col >= g.cols) break;
+                    float v[32];
+                    ld_acc(acc + c, v);
+                    if (col + 32 > g.cols) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (col + j >= g.cols) v[j] = -INFINITY;
+                    }
+                    if (t >= col && t < col + 32 && t < g.cols) {
+                        float z = v[0];
+#pragma unroll
+                        for (int j = 1; j < 32; ++j) z = (int)t - col == j ? v[j] : z;
+                        p.target_logit[row] = z;
+                    }
+                    float top = v[0];
+#pragma unroll
+                    for (int j = 1; j < 32; ++j) top = fmaxf(top, v[j]);
+                    top = fmaxf(top, ref);
+                    top = fabsf(top) < INFINITY ? top : 0.f;
+                    float part[4] = {sum * ex2((ref - top) * LOG2E), 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) part[j & 3] += ex2((v[j] - top) * LOG2E);
+                    sum = (part[0] + part[1]) + (part[2] + part[3]);
+                    ref = top;
+                }
+                if (in) p.stats[(size_t)tn * g.rows + row] = make_float2(ref, sum);
+            } else {
+                const float lse = in ? p.lse[row] : 0.f;
+                long long t = in ? p.targets[row] : -1;
+                float w = t >= 0 && t < p.vocab ? 1.f : 0.f;
+                if (w != 0.f && p.dloss) w = p.dloss[row];
+                t = t >= 0 && t < p.vocab ? t - p.first_col : -1;
+                for (int c = 0; c < BN; c += 64) {
+                    const int col = tn * BN + c;
+                    if (col >= g.cols) break;
+                    const uint32_t sl = take_slab();
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        float v[32];
+                        ld_acc(acc + c + 32 * half, v);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = ex2((v[j] - lse) * LOG2E);
+                        const long long at = t - (col + 32 * half);
+                        if (at >= 0 && at < 32) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if ((int)at == j) v[j] -= 1.f;
+                        }
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] *= w;
+                        if (col + 32 * half + 32 > g.cols) {          // (columns that fill up a row of the tensor: an operand, so zero)
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (col + 32 * half + j >= g.cols) v[j] = 0.f;
+                        }
+                        put_bf16(sl, lane, half, v);
+                    }
+                    send(&p.out[g.out], col, sl);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if constexpr (CG == 2) arrive_cluster_if(map_to_leader(bar(BAR_ACC_EMPTY + set)), lane == 0);
+            else mbar_arrive_if(bar(BAR_ACC_EMPTY + set), lane == 0);
+        }
+        if (lane == 0) bulk_wait<0>();
+        __syncwarp();
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync();            // neither CTA's memory goes while the other's products or arrivals may reach it
+    if (warp == 1) {
+        tc_fence_after();
+        if constexpr (CG == 2) tmem_dealloc_pair(tmem, 512);
+        else tmem_dealloc(tmem, 512);
+    }
+}
+
+// [rows][C] fp32 tensor, box = 32 rows x 32 columns (128 bytes), 128-byte swizzle
+inline bool make_map_f32(CUtensorMap* tm, const void* base, long long rows, long long C)
+{
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)C, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)C * 4};
+    cuuint32_t box[2] = {32, 32};
+    cuuint32_t estr[2] = {1, 1};
+    return enc(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// operand in 64 x 64 tiles; result in 32-row slabs of 64 columns.  (A row is 2 C bytes: C a multiple of 8.)
+inline bool in_map(CUtensorMap* tm, const void* base, long long rows, long long C) { return make_map(tm, base, rows, C, 64); }
+inline bool out_map(CUtensorMap* tm, const void* base, long long rows, long long C) { return make_map(tm, base, rows, C, 32); }
+
+inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+// A group whose result is rows x cols, in tiles of 128*cg rows and `width` columns.
+inline Group make_group(int cg, long long rows, long long cols, int width)
+{
+    Group g = {};
+    g.tiles_m = (int)ceil_div(rows, 128 * cg);
+    g.tiles_n = (int)ceil_div(cols, width);
+    g.rows = (int)rows;
+    g.cols = (int)cols;
+    return g;
+}
+inline void add_group(GemmParams& p, const Group& g)
+{
+    p.g[p.n_groups] = g;
+    p.g[p.n_groups].first = p.n_tiles;
+    p.n_tiles += g.tiles_m * g.tiles_n;
+    ++p.n_groups;
+}
+
+template <int CG, Epilogue EPI>
+inline cudaError_t launch_one(const GemmParams& p, int n_sm, int dev, cudaStream_t st)
+{
+    static PerDeviceFlag attr_set;
+    if (!attr_set.is_set(dev)) {
+        const cudaError_t e = cudaFuncSetAttribute(pair_gemm_kernel<CG, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+        if (e != cudaSuccess) return e;
+        attr_set.set(dev);
+    }
+    const int units = n_sm / CG;
+    const unsigned grid = (unsigned)(CG * (p.n_tiles < units ? p.n_tiles : units));
+    return launch_pdl_cluster(pair_gemm_kernel<CG, EPI>, grid, THREADS, SMEM, CG, st, p);
+}
+template <Epilogue EPI>
+inline gf_status_t launch(int cg, const GemmParams& p, cudaStream_t st, std::atomic<uint64_t>* launches)
+{
+    const int n_sm = sm_count(), dev = current_device();
+    if (n_sm < 2 || dev < 0) return GF_ERR_CUDA;
+    const cudaError_t e = cg == 2 ? launch_one<2, EPI>(p, n_sm, dev, st) : launch_one<1, EPI>(p, n_sm, dev, st);
+    launches->fetch_add(1, std::memory_order_relaxed);
+    return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
+}
+
+}  // namespace pg
+}  // namespace gf

@@ -1,0 +1,165 @@
+// Cross entropy of a linear layer over a vocabulary, without the logits: for every row
+//     z = x W^T,   lse = log sum_v exp z_v,   loss = lse - z_target        (W: [V][D]; loss 0 where there is no target)
+// and its gradient, with P = (softmax z - [v is the target]) dloss,
+//     dx = P W,   dW = P^T x.
+//
+// Forward: pair_gemm_kernel makes 256 (128) columns of logits at a time and keeps of each row a reference value and the sum of
+// exponentials over it; a second kernel joins them.  Gradient: pieces of the vocabulary, each one launch that computes the
+// piece's logits again and writes its columns of P in bf16 (they are an operand of two products whose results are bf16), and one
+// that computes the piece's rows of dW and adds its part of dx, kept in fp32 until the last piece.
+#pragma once
+#include "gated_linear.cuh"
+
+namespace gf {
+namespace vl {
+
+using namespace pg;
+using gl::choose_cg;
+using gl::segment;
+
+constexpr int JOIN_WARPS = 16;
+
+// stats [tiles][rows] -> lse, loss.  A block takes 32 rows, its warps every JOIN_WARPS-th tile.
+__global__ void __launch_bounds__(32 * JOIN_WARPS) join_kernel(const float2* __restrict__ stats, const float* __restrict__ target_logit,
+                                                               const long long* __restrict__ targets, long long vocab, int tiles, int rows,
+                                                               float* __restrict__ loss, float* __restrict__ lse)
+{
+    __shared__ float2 part[JOIN_WARPS][32];
+    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x * 32 + lane;
+    float ref = -INFINITY, sum = 0.f;
+    // (a tile's reference is finite; a warp without tiles keeps -inf, whose factor below is exp(-inf) = 0)
+    auto join = [&](float2 o) {
+        const float top = fmaxf(ref, o.x);
+        sum = sum * __expf(ref - top) + o.y * __expf(o.x - top);
+        ref = top;
+    };
+    if (row < rows) {
+        int t = warp;
+        for (; t + 3 * JOIN_WARPS < tiles; t += 4 * JOIN_WARPS) {
+            float2 o[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) o[q] = stats[(size_t)(t + q * JOIN_WARPS) * rows + row];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) join(o[q]);
+        }
+        for (; t < tiles; t += JOIN_WARPS) join(stats[(size_t)t * rows + row]);
+    }
+    part[warp][lane] = make_float2(ref, sum);
+    __syncthreads();
+    if (warp == 0 && row < rows) {
+        for (int w = 1; w < JOIN_WARPS && w < tiles; ++w) join(part[w][lane]);
+        const float l = ref + logf(sum);
+        const long long t = targets[row];
+        lse[row] = l;
+        loss[row] = t >= 0 && t < vocab ? l - target_logit[row] : 0.f;
+    }
+}
+
+inline int forward_cg(long long rows, long long cols, int n_sm)
+{
+    return choose_cg(ceil_div(rows, 256) * ceil_div(cols, 256), ceil_div(rows, 128) * ceil_div(cols, 128), n_sm);
+}
+
+// Columns of P that the gradient holds at a time: 256 MB of them, between 1024 and the vocabulary, in equal pieces.
+inline long long piece_cols(long long rows, long long V)
+{
+    long long most = (128LL << 20) / rows / 256 * 256;
+    if (most < 1024) most = 1024;
+    const long long n = ceil_div(V, most);
+    return ceil_div(ceil_div(V, n), 256) * 256;
+}
+
+}  // namespace vl
+
+inline size_t round_256(size_t n) { return (n + 255) & ~(size_t)255; }
+// Forward: the statistics of every 128 columns, and the targets' logits.
+inline size_t vocab_loss_bytes(long long rows, long long V) { return round_256((size_t)rows * pg::ceil_div(V, 128) * sizeof(float2)) + (size_t)rows * 4; }
+// Gradient: a piece of P and, where there are several, the sums of dx.
+inline size_t vocab_loss_backward_bytes(long long rows, int D, long long V)
+{
+    const long long c = vl::piece_cols(rows, V);
+    return round_256((size_t)rows * c * 2) + (c < V ? (size_t)rows * D * 4 : 0);
+}
+
+inline gf_status_t vocab_loss(const __nv_bfloat16* x, const __nv_bfloat16* w, const long long* targets, float* loss, float* lse, long long rows,
+                              int D, long long V, void* ws, cudaStream_t st, std::atomic<uint64_t>* launches)
+{
+    using namespace vl;
+    const int n_sm = sm_count();
+    if (n_sm < 2) return GF_ERR_CUDA;
+    const int cg = forward_cg(rows, V, n_sm);
+    GemmParams p = {};
+    if (!in_map(&p.in[0], x, rows, D) || !in_map(&p.in[1], w, V, D)) return GF_ERR_CUDA;
+    Group g = make_group(cg, rows, V, 128 * cg);
+    g.n_seg = 1;
+    g.seg[0] = segment(0, false, 1, false, D);
+    add_group(p, g);
+    p.targets = targets;
+    p.vocab = V;
+    p.stats = static_cast<float2*>(ws);
+    p.target_logit = reinterpret_cast<float*>(static_cast<char*>(ws) + round_256((size_t)rows * ceil_div(V, 128) * sizeof(float2)));
+    const gf_status_t s = launch<EPI_LSE>(cg, p, st, launches);
+    if (s != GF_OK) return s;
+    const cudaError_t e = launch_pdl(join_kernel, (unsigned)ceil_div(rows, 32), 32 * JOIN_WARPS, 0, st, p.stats, p.target_logit, targets, V, g.tiles_n,
+                                     (int)rows, loss, lse);
+    launches->fetch_add(1, std::memory_order_relaxed);
+    return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
+}
+
+inline gf_status_t vocab_loss_backward(const __nv_bfloat16* x, const __nv_bfloat16* w, const long long* targets, const float* lse, const float* dloss,
+                                       __nv_bfloat16* dx, __nv_bfloat16* dw, long long rows, int D, long long V, void* ws, cudaStream_t st,
+                                       std::atomic<uint64_t>* launches)
+{
+    using namespace vl;
+    const int n_sm = sm_count();
+    if (n_sm < 2) return GF_ERR_CUDA;
+    const long long step = piece_cols(rows, V);
+    __nv_bfloat16* P = static_cast<__nv_bfloat16*>(ws);
+    float* sums = reinterpret_cast<float*>(static_cast<char*>(ws) + round_256((size_t)rows * step * 2));
+    for (long long v0 = 0; v0 < V; v0 += step) {
+        const long long cols = V - v0 < step ? V - v0 : step;
+        const long long pitch = (cols + 7) / 8 * 8;               // (a row of a tensor map is a multiple of 16 bytes; the last columns are zero)
+        const __nv_bfloat16* wp = w + (size_t)v0 * D;
+        {
+            GemmParams p = {};
+            const int cg = forward_cg(rows, cols, n_sm);
+            if (!in_map(&p.in[0], x, rows, D) || !in_map(&p.in[1], wp, cols, D) || !out_map(&p.out[0], P, rows, pitch)) return GF_ERR_CUDA;
+            Group g = make_group(cg, rows, cols, 128 * cg);
+            g.n_seg = 1;
+            g.seg[0] = segment(0, false, 1, false, D);
+            add_group(p, g);
+            p.targets = targets;
+            p.vocab = V;
+            p.first_col = (int)v0;
+            p.lse = lse;
+            p.dloss = dloss;
+            const gf_status_t s = launch<EPI_PROB>(cg, p, st, launches);
+            if (s != GF_OK) return s;
+        }
+        GemmParams p = {};
+        const bool first = v0 == 0, last = v0 + step >= V;
+        if (!in_map(&p.in[0], P, rows, pitch) || !in_map(&p.in[1], wp, cols, D) || !in_map(&p.in[2], x, rows, D) || !out_map(&p.out[1], dw + (size_t)v0 * D, cols, D) ||
+            !(last ? out_map(&p.out[0], dx, rows, D) : make_map_f32(&p.out[0], sums, rows, D)))
+            return GF_ERR_CUDA;
+        const int cg = choose_cg(ceil_div(rows, 256) * ceil_div(D, 256) + ceil_div(cols, 256) * ceil_div(D, 256),
+                                 ceil_div(rows, 128) * ceil_div(D, 128) + ceil_div(cols, 128) * ceil_div(D, 128), n_sm);
+        Group gx = make_group(cg, rows, D, 128 * cg), gw = make_group(cg, cols, D, 128 * cg);
+        gx.n_seg = gw.n_seg = 1;
+        gx.seg[0] = segment(0, false, 1, true, cols);
+        gx.out = 0;
+        gx.mode = last ? (first ? OUT_BF16 : OUT_BF16_ADD) : (first ? OUT_F32 : OUT_F32_ADD);
+        gx.part = sums;
+        gw.seg[0] = segment(0, true, 2, true, rows);
+        gw.out = 1;
+        gw.mode = OUT_BF16;
+        // the deeper products first: the round that ends unevenly is the shorter one's
+        add_group(p, cols >= rows ? gx : gw);
+        add_group(p, cols >= rows ? gw : gx);
+        const gf_status_t s = launch<EPI_STORE>(cg, p, st, launches);
+        if (s != GF_OK) return s;
+    }
+    return GF_OK;
+}
+
+}  // namespace gf
