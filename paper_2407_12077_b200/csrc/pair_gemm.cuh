@@ -17,11 +17,14 @@
 //
 //   warp 0      TMA producer: 64 contraction indices of A and B (16 KB each per CTA) per stage of a six-stage ring
 //   warp 1      tensor-memory allocation; an elected lane of the leading CTA issues the four products of a stage
-//   warps 2-5   epilogue: a lane owns a row of the tile, 32 columns at a time
+//   warps 2-9   epilogue: a lane owns a row of the tile, 32 columns at a time, two warps sharing a row's columns out in blocks of 64
 // Every wait is bounded (status flag and abort as in the prefill kernel); a pair's CTAs meet before either leaves.
 #pragma once
 #include "key_compress.cuh"
 #include "wkv6_chunked.cuh"
+
+#include <float.h>
+#include <type_traits>
 
 namespace gf {
 namespace pg {
@@ -30,11 +33,12 @@ using namespace ck;                                   // PTX wrappers, descripto
 using kc::cluster_sync;
 using kc::tmem_ld_row32;
 
-constexpr int THREADS = 192;
+constexpr int N_EPI = 8;                              // epilogue warps: two per tensor-memory sub-partition
+constexpr int THREADS = 64 + 32 * N_EPI;
 constexpr int NSTAGE = 6;
 constexpr int STAGE_BYTES = 4 * TILE;                 // 128 x 64 of A, 128 x 64 of B
-constexpr int OFF_SLAB = NSTAGE * STAGE_BYTES;        // [4 warps][2][32 rows x 128 B]
-constexpr int OFF_MISC = OFF_SLAB + 4 * 2 * 4096;     // abort word, wait limit, tensor-memory address, barriers
+constexpr int OFF_SLAB = NSTAGE * STAGE_BYTES;        // [N_EPI warps][32 rows x 128 B]
+constexpr int OFF_MISC = OFF_SLAB + N_EPI * 4096;     // abort word, wait limit, tensor-memory address, barriers
 constexpr int SMEM = OFF_MISC + 256 + 1024;           // + slack for manual 1024-byte alignment
 static_assert(SMEM <= 232448, "shared memory budget of one sm_100 CTA");
 enum { BAR_FULL = 0, BAR_EMPTY = NSTAGE, BAR_ACC_FULL = 2 * NSTAGE, BAR_ACC_EMPTY = BAR_ACC_FULL + 2, BAR_DRAIN = BAR_ACC_EMPTY + 2, N_BARS };
@@ -83,7 +87,7 @@ struct GemmParams {
     const long long* targets;
     long long vocab;                // a target outside [0, vocab) is none
     int first_col;                  // the vocabulary's index of this launch's first column
-    float2* stats;                  // [tiles_n][rows] (reference value, sum of exponentials over it)
+    float2* stats;                  // [2 tiles_n][rows] (reference value, sum of exponentials over it) of each half of a tile's columns
     float* target_logit;
     const float* lse;
     const float* dloss;             // or nullptr: ones
@@ -146,34 +150,43 @@ __device__ __forceinline__ uint32_t instr_desc(int m, int n, bool a_mn, bool b_m
 }
 
 // ---------------------------------------------------------------- activations
-// 1 / (1 + exp(-|a|)) and exp(-|a|): both sides of the sigmoid from an exponential that cannot overflow
-__device__ __forceinline__ float act_value(int act, float a)
+template <int ACT> __device__ __forceinline__ float act_value(float a)
 {
-    if (act == ACT_RELU2) {
-        const float r = fmaxf(a, 0.f);
-        return a != a ? a : r * r;
+    if constexpr (ACT == ACT_RELU2) {
+        const float r = a != a ? a : fmaxf(a, 0.f);
+        return r * r;
+    } else if constexpr (ACT == ACT_GELU) {
+        return a * (0.5f * erfcf(a * -0.70710678f));
+    } else {
+        const float s = __fdividef(1.f, 1.f + __expf(-a));
+        return ACT == ACT_SIGMOID ? s : a * s;
     }
-    if (act == ACT_GELU) return a * (0.5f * erfcf(a * -0.70710678f));
-    const float s = __fdividef(1.f, 1.f + __expf(-a));
-    return act == ACT_SIGMOID ? s : a * s;
 }
-// value and derivative
-__device__ __forceinline__ void act_grad(int act, float a, float& f, float& df)
+// value and derivative; the sigmoid and one minus it from an exponential that cannot overflow, without cancellation
+template <int ACT> __device__ __forceinline__ void act_grad(float a, float& f, float& df)
 {
-    if (act == ACT_RELU2) {
+    if constexpr (ACT == ACT_RELU2) {
         const float r = a != a ? a : fmaxf(a, 0.f);
         f = r * r;
         df = 2.f * r;
-    } else if (act == ACT_GELU) {
+    } else if constexpr (ACT == ACT_GELU) {
         const float phi = 0.5f * erfcf(a * -0.70710678f);
         f = a * phi;
         df = fmaf(a * 0.39894228f, __expf(-0.5f * a * a), phi);
     } else {
-        const float e = __expf(-fabsf(a)), r = __fdividef(1.f, 1.f + e);
-        const float s = a >= 0.f ? r : e * r, t = a >= 0.f ? e * r : r;      // t = 1 - s without cancellation
-        f = act == ACT_SIGMOID ? s : a * s;
-        df = act == ACT_SIGMOID ? s * t : s * fmaf(a, t, 1.f);
+        const float e = __expf(-fabsf(a)), r = __fdividef(1.f, 1.f + e), er = e * r;
+        const float s = a >= 0.f ? r : er, t = a >= 0.f ? er : r;
+        f = ACT == ACT_SIGMOID ? s : a * s;
+        df = ACT == ACT_SIGMOID ? s * t : s * fmaf(a, t, 1.f);
     }
+}
+// f(std::integral_constant<int, act>): one branch for all values of a lane
+template <typename F> __device__ __forceinline__ void by_act(int act, F&& f)
+{
+    if (act == ACT_SIGMOID) f(std::integral_constant<int, ACT_SIGMOID>());
+    else if (act == ACT_RELU2) f(std::integral_constant<int, ACT_RELU2>());
+    else if (act == ACT_SILU) f(std::integral_constant<int, ACT_SILU>());
+    else f(std::integral_constant<int, ACT_GELU>());
 }
 
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
@@ -232,7 +245,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(BAR_ACC_FULL + i), 1);
-            mbar_init(bar(BAR_ACC_EMPTY + i), 4 * CG);
+            mbar_init(bar(BAR_ACC_EMPTY + i), N_EPI * CG);
         }
         mbar_init(bar(BAR_DRAIN), 1);
         sts32(abort_flag, 0u);
@@ -354,8 +367,9 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
     } else {
         // ============================== epilogue warps ==============================
         const int sp = warp & 3;                      // tensor-memory sub-partition: accumulator rows 32*sp .. 32*sp+31
-        const uint32_t slabs = sbase + OFF_SLAB + (warp - 2) * 2 * 4096;
-        int ti = 0, sb = 0;
+        const int part = (warp - 2) >> 2;             // takes the row's blocks of 64 columns part, part + 2, ..
+        const uint32_t sl = sbase + OFF_SLAB + (warp - 2) * 4096;
+        int ti = 0;
         for (int tile = unit; tile < p.n_tiles; tile += units, ++ti) {
             int gi, tm, tn;
             tile_at(p, tile, gi, tm, tn);
@@ -366,48 +380,42 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
             const uint32_t acc = tmem + ((uint32_t)(32 * sp) << 16) + ACC_COLS * set;
             const int row0 = tm * 128 * CG + 128 * (int)rank + 32 * sp, row = row0 + lane;
             const bool in = row < g.rows;
-            // a slab that no store is reading any more
+            // the slab, once no store is reading it any more
             auto take_slab = [&]() {
-                if (lane == 0) bulk_wait_read<1>();
+                if (lane == 0) bulk_wait_read<0>();
                 __syncwarp();
-                const uint32_t sl = slabs + 4096 * sb;
-                sb ^= 1;
-                return sl;
             };
-            auto send = [&](const CUtensorMap* m, int col, uint32_t sl) {
+            auto send = [&](const CUtensorMap* m, int col) {
                 fence_proxy_async();
                 __syncwarp();
-                if (lane == 0) {                      // (a group each time, if an empty one: take_slab() counts them)
-                    if (row0 < g.rows) tma_store_2d(m, col, row0, sl);
+                if (lane == 0 && row0 < g.rows) {
+                    tma_store_2d(m, col, row0, sl);
                     bulk_commit();
                 }
             };
             if constexpr (EPI == EPI_STORE) {
-                if (g.mode == OUT_F32 || g.mode == OUT_F32_ADD) {
-                    for (int c = 0; c < BN; c += 32) {
-                        const int col = tn * BN + c;
-                        if (col >= g.cols) break;
-                        float v[32];
-                        ld_acc(acc + c, v);
-                        const uint32_t sl = take_slab();
+                for (int c = 64 * part; c < BN; c += 128) {
+                    const int col = tn * BN + c;
+                    if (col >= g.cols) break;
+                    if (g.mode == OUT_F32 || g.mode == OUT_F32_ADD) {
 #pragma unroll
-                        for (int q = 0; q < 8; ++q)
-                            sts128(sl + swz(lane, q << 4), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
-                        fence_proxy_async();
-                        __syncwarp();
-                        if (lane == 0) {
-                            if (row0 < g.rows) {
-                                if (g.mode == OUT_F32) tma_store_2d(&p.out[g.out], col, row0, sl);
-                                else tma_reduce_add_2d(&p.out[g.out], col, row0, sl);
+                        for (int half = 0; half < 2; ++half) {
+                            float v[32];
+                            ld_acc(acc + c + 32 * half, v);
+                            take_slab();
+#pragma unroll
+                            for (int q = 0; q < 8; ++q)
+                                sts128(sl + swz(lane, q << 4), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
+                            fence_proxy_async();
+                            __syncwarp();
+                            if (lane == 0 && row0 < g.rows && col + 32 * half < g.cols) {
+                                if (g.mode == OUT_F32) tma_store_2d(&p.out[g.out], col + 32 * half, row0, sl);
+                                else tma_reduce_add_2d(&p.out[g.out], col + 32 * half, row0, sl);
+                                bulk_commit();
                             }
-                            bulk_commit();
                         }
-                    }
-                } else {
-                    for (int c = 0; c < BN; c += 64) {
-                        const int col = tn * BN + c;
-                        if (col >= g.cols) break;
-                        const uint32_t sl = take_slab();
+                    } else {
+                        take_slab();
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
                             float v[32];
@@ -423,21 +431,23 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                             }
                             put_bf16(sl, lane, half, v);
                         }
-                        send(&p.out[g.out], col, sl);
+                        send(&p.out[g.out], col);
                     }
                 }
             } else if constexpr (EPI == EPI_GATE) {
                 const int width = p.gated ? HW : BN;
-                for (int c = 0; c < width; c += 64) {
+                for (int c = 64 * part; c < width; c += 128) {
                     const int col = tn * width + c;
                     if (col >= g.cols) break;
-                    const uint32_t sl = take_slab();
+                    take_slab();
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         float a[32];
                         ld_acc(acc + c + 32 * half, a);
+                        by_act(p.act, [&](auto k) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) a[j] = act_value(p.act, a[j]);
+                            for (int j = 0; j < 32; ++j) a[j] = act_value<decltype(k)::value>(a[j]);
+                        });
                         if (p.gated) {
                             float b[32];
                             ld_acc(acc + HW + c + 32 * half, b);
@@ -446,15 +456,15 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                         }
                         put_bf16(sl, lane, half, a);
                     }
-                    send(&p.out[0], col, sl);
+                    send(&p.out[0], col);
                 }
             } else if constexpr (EPI == EPI_GATE_GRAD) {
                 const int width = p.gated ? HW : BN;
-                for (int c = 0; c < width; c += 64) {
+                for (int c = 64 * part; c < width; c += 128) {
                     const int col = tn * width + c;
                     if (col >= g.cols) break;
-                    if (lane == 0) bulk_wait_read<0>();
-                    __syncwarp();
+                    take_slab();
+                    uint32_t later[2][16];            // db, in bf16, until da has left the slab
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         uint32_t d[16];
@@ -464,29 +474,50 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                             const uint4 u = in && col + 32 * half + 8 * q < g.cols ? __ldg(reinterpret_cast<const uint4*>(src) + q) : make_uint4(0u, 0u, 0u, 0u);
                             d[4 * q] = u.x; d[4 * q + 1] = u.y; d[4 * q + 2] = u.z; d[4 * q + 3] = u.w;
                         }
-                        float a[32], b[32];
+                        auto dy = [&](int j) { return __uint_as_float(j & 1 ? d[j / 2] & 0xffff0000u : d[j / 2] << 16); };
+                        float a[32];
                         ld_acc(acc + c + 32 * half, a);
-                        if (p.gated) ld_acc(acc + HW + c + 32 * half, b);
+                        if (p.gated) {
+                            float b[32];
+                            ld_acc(acc + HW + c + 32 * half, b);
+                            by_act(p.act, [&](auto k) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const float dy = __uint_as_float(j & 1 ? d[j / 2] & 0xffff0000u : d[j / 2] << 16);
-                            float f, df;
-                            act_grad(p.act, a[j], f, df);
-                            a[j] = p.gated ? dy * b[j] * df : dy * df;
-                            b[j] = dy * f;
+                                for (int j = 0; j < 32; ++j) {
+                                    float f, df;
+                                    act_grad<decltype(k)::value>(a[j], f, df);
+                                    a[j] = dy(j) * b[j] * df;
+                                    b[j] = dy(j) * f;
+                                }
+                            });
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) later[half][j] = pack_bf16(b[2 * j], b[2 * j + 1]);
+                        } else {
+                            by_act(p.act, [&](auto k) {
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) {
+                                    float f, df;
+                                    act_grad<decltype(k)::value>(a[j], f, df);
+                                    a[j] = dy(j) * df;
+                                }
+                            });
                         }
-                        put_bf16(slabs, lane, half, a);
-                        if (p.gated) put_bf16(slabs + 4096, lane, half, b);
+                        put_bf16(sl, lane, half, a);
                     }
-                    send(&p.out[0], col, slabs);
-                    if (p.gated) send(&p.out[1], col, slabs + 4096);
+                    send(&p.out[0], col);
+                    if (p.gated) {
+                        take_slab();
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            sts128(sl + swz(lane, q << 4), later[q / 4][4 * (q % 4)], later[q / 4][4 * (q % 4) + 1], later[q / 4][4 * (q % 4) + 2], later[q / 4][4 * (q % 4) + 3]);
+                        send(&p.out[1], col);
+                    }
                 }
             } else if constexpr (EPI == EPI_LSE) {
-                // exp is taken of differences to a reference, the largest value so far (0 instead of an infinite one: the sum is then
-                // infinite, or zero, by itself); a NaN reaches the sum through its own exponential
-                float ref = -INFINITY, sum = 0.f;
+                // a warp takes half of the tile's columns.  exp is taken of differences to a reference, the largest value so far (0
+                // instead of an infinite one: the sum is then infinite, or zero, by itself); a NaN reaches the sum through its own exponential
+                float ref = -FLT_MAX, sum = 0.f;
                 const long long t = in ? p.targets[row] : -1;
-                for (int c = 0; c < BN; c += 32) {
+                for (int c = HW * part; c < HW * part + HW; c += 32) {
                     const int col = tn * BN + c;
                     if (col >= g.cols) break;
                     float v[32];
@@ -505,25 +536,25 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                     float top = v[0];
 #pragma unroll
                     for (int j = 1; j < 32; ++j) top = fmaxf(top, v[j]);
-                    top = fmaxf(top, ref);
+                    top = c == HW * part ? top : fmaxf(top, ref);
                     top = fabsf(top) < INFINITY ? top : 0.f;
-                    float part[4] = {sum * ex2((ref - top) * LOG2E), 0.f, 0.f, 0.f};
+                    float s4[4] = {sum * ex2((ref - top) * LOG2E), 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) part[j & 3] += ex2((v[j] - top) * LOG2E);
-                    sum = (part[0] + part[1]) + (part[2] + part[3]);
+                    for (int j = 0; j < 32; ++j) s4[j & 3] += ex2((v[j] - top) * LOG2E);
+                    sum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
                     ref = top;
                 }
-                if (in) p.stats[(size_t)tn * g.rows + row] = make_float2(ref, sum);
+                if (in) p.stats[(size_t)(2 * tn + part) * g.rows + row] = make_float2(ref, sum);
             } else {
                 const float lse = in ? p.lse[row] : 0.f;
                 long long t = in ? p.targets[row] : -1;
                 float w = t >= 0 && t < p.vocab ? 1.f : 0.f;
                 if (w != 0.f && p.dloss) w = p.dloss[row];
                 t = t >= 0 && t < p.vocab ? t - p.first_col : -1;
-                for (int c = 0; c < BN; c += 64) {
+                for (int c = 64 * part; c < BN; c += 128) {
                     const int col = tn * BN + c;
                     if (col >= g.cols) break;
-                    const uint32_t sl = take_slab();
+                    take_slab();
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         float v[32];
@@ -545,7 +576,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                         }
                         put_bf16(sl, lane, half, v);
                     }
-                    send(&p.out[g.out], col, sl);
+                    send(&p.out[g.out], col);
                 }
             }
             tc_fence_before();

@@ -3,8 +3,8 @@
 // and its gradient, with P = (softmax z - [v is the target]) dloss,
 //     dx = P W,   dW = P^T x.
 //
-// Forward: pair_gemm_kernel makes 256 (128) columns of logits at a time and keeps of each row a reference value and the sum of
-// exponentials over it; a second kernel joins them.  Gradient: pieces of the vocabulary, each one launch that computes the
+// Forward: pair_gemm_kernel makes 256 (128) columns of logits at a time and keeps of each row and half of them a reference value and the
+// sum of exponentials over it; a second kernel joins them.  Gradient: pieces of the vocabulary, each one launch that computes the
 // piece's logits again and writes its columns of P in bf16 (they are an operand of two products whose results are bf16), and one
 // that computes the piece's rows of dW and adds its part of dx, kept in fp32 until the last piece.
 #pragma once
@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) join_kernel(const float2* __r
     asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x * 32 + lane;
     float ref = -INFINITY, sum = 0.f;
-    // (a tile's reference is finite; a warp without tiles keeps -inf, whose factor below is exp(-inf) = 0)
+    // (references are finite, so a first one's factor below is exp(-inf) = 0)
     auto join = [&](float2 o) {
         const float top = fmaxf(ref, o.x);
         sum = sum * __expf(ref - top) + o.y * __expf(o.x - top);
@@ -73,8 +73,9 @@ inline long long piece_cols(long long rows, long long V)
 }  // namespace vl
 
 inline size_t round_256(size_t n) { return (n + 255) & ~(size_t)255; }
-// Forward: the statistics of every 128 columns, and the targets' logits.
-inline size_t vocab_loss_bytes(long long rows, long long V) { return round_256((size_t)rows * pg::ceil_div(V, 128) * sizeof(float2)) + (size_t)rows * 4; }
+// Forward: the statistics of every half tile of columns (64 at least), and the targets' logits.
+inline size_t vocab_stats_bytes(long long rows, long long V) { return round_256((size_t)rows * 2 * pg::ceil_div(V, 128) * sizeof(float2)); }
+inline size_t vocab_loss_bytes(long long rows, long long V) { return vocab_stats_bytes(rows, V) + (size_t)rows * 4; }
 // Gradient: a piece of P and, where there are several, the sums of dx.
 inline size_t vocab_loss_backward_bytes(long long rows, int D, long long V)
 {
@@ -98,10 +99,10 @@ inline gf_status_t vocab_loss(const __nv_bfloat16* x, const __nv_bfloat16* w, co
     p.targets = targets;
     p.vocab = V;
     p.stats = static_cast<float2*>(ws);
-    p.target_logit = reinterpret_cast<float*>(static_cast<char*>(ws) + round_256((size_t)rows * ceil_div(V, 128) * sizeof(float2)));
+    p.target_logit = reinterpret_cast<float*>(static_cast<char*>(ws) + vocab_stats_bytes(rows, V));
     const gf_status_t s = launch<EPI_LSE>(cg, p, st, launches);
     if (s != GF_OK) return s;
-    const cudaError_t e = launch_pdl(join_kernel, (unsigned)ceil_div(rows, 32), 32 * JOIN_WARPS, 0, st, p.stats, p.target_logit, targets, V, g.tiles_n,
+    const cudaError_t e = launch_pdl(join_kernel, (unsigned)ceil_div(rows, 32), 32 * JOIN_WARPS, 0, st, p.stats, p.target_logit, targets, V, 2 * g.tiles_n,
                                      (int)rows, loss, lse);
     launches->fetch_add(1, std::memory_order_relaxed);
     return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
