@@ -39,12 +39,12 @@ inline int choose_cg(long long large, long long small, int n_sm)
 }
 
 // Both products of every column (maps 0: x, 1: w, 2: w2, 3: x2; all as they lie in memory, weights [K][F]).
-inline bool products(GemmParams& p, int cg, const Shape& s, const __nv_bfloat16* x, const __nv_bfloat16* w, const __nv_bfloat16* x2, const __nv_bfloat16* w2)
+inline bool products(GemmParams& p, int cg, bool wide, const Shape& s, const __nv_bfloat16* x, const __nv_bfloat16* w, const __nv_bfloat16* x2, const __nv_bfloat16* w2)
 {
     const bool gated = s.K2 > 0;
     if (!in_map(&p.in[0], x, s.rows, s.K1) || !in_map(&p.in[1], w, s.K1, s.F)) return false;
     if (gated && (!in_map(&p.in[2], w2, s.K2, s.F) || !in_map(&p.in[3], x2, s.rows, s.K2))) return false;
-    Group g = make_group(cg, s.rows, s.F, gated ? 64 * cg : 128 * cg);
+    Group g = make_group(cg, s.rows, s.F, gated && !wide ? 64 * cg : 128 * cg);
     if (!gated) {
         g.n_seg = 1;
         g.seg[0] = segment(0, false, 1, true, s.K1);
@@ -53,17 +53,31 @@ inline bool products(GemmParams& p, int cg, const Shape& s, const __nv_bfloat16*
         g.seg[0] = segment(0, false, 1, true, s.K1, true, B_DUAL);
     } else {
         g.n_seg = 2;
-        g.seg[0] = segment(0, false, 1, true, s.K1, true, B_HALF, false);
-        g.seg[1] = segment(3, false, 2, true, s.K2, true, B_HALF, true);
+        g.seg[0] = segment(0, false, 1, true, s.K1, true, wide ? B_WHOLE : B_HALF, false);
+        g.seg[1] = segment(3, false, 2, true, s.K2, true, wide ? B_WHOLE : B_HALF, true);
     }
     p.gated = gated;
     add_group(p, g);
     return true;
 }
-inline int forward_cg(const Shape& s, int n_sm)
+// The launch of both products: pairs of CTAs or single ones; *wide: a whole accumulator for each product (see pair_gemm.cuh).
+// Rounds of tiles times the time of one, in steps of a pair on 256 x 256: half tiles take 0.64 of one (16384 rows, 2048 and 7168 deep
+// -> 2048: 520 us, wide 408; 8192 rows, twice 512 -> 8192: 149, wide 126), a wide tile about two more for what its epilogue leaves
+// (8192 rows, twice 256 -> 8192: 103 and 101); where wide tiles are too few, half ones win (2048 rows, 768 and 2688 -> 768:
+// 20 us, wide 25).
+inline int forward_cg(const Shape& s, int n_sm, bool* wide)
 {
-    const int w = s.K2 > 0 ? 64 : 128;
-    return choose_cg(ceil_div(s.rows, 256) * ceil_div(s.F, 2 * w), ceil_div(s.rows, 128) * ceil_div(s.F, w), n_sm);
+    const long long m2 = ceil_div(s.rows, 256), m1 = ceil_div(s.rows, 128);
+    *wide = false;
+    if (s.K2 == 0 || s.same) {
+        const int w = s.K2 > 0 ? 64 : 128;
+        return choose_cg(m2 * ceil_div(s.F, 2 * w), m1 * ceil_div(s.F, w), n_sm);
+    }
+    const long long steps = ceil_div(s.K1, 64) + ceil_div(s.K2, 64);
+    const long long t_wide = ceil_div(m2 * ceil_div(s.F, 256), n_sm / 2) * (steps + 2) * 100;
+    const long long t_half = ceil_div(m2 * ceil_div(s.F, 128), n_sm / 2) * steps * 64, t_one = ceil_div(m1 * ceil_div(s.F, 64), n_sm) * steps * 45;
+    *wide = t_wide <= t_half && t_wide <= t_one;
+    return *wide || t_half <= t_one ? 2 : 1;
 }
 
 }  // namespace gl
@@ -75,9 +89,10 @@ inline gf_status_t gated_linear(const __nv_bfloat16* x, const __nv_bfloat16* w, 
     if (n_sm < 2) return GF_ERR_CUDA;
     pg::GemmParams p = {};
     p.act = act;
-    const int cg = gl::forward_cg(s, n_sm);
-    if (!gl::products(p, cg, s, x, w, x2, w2) || !pg::out_map(&p.out[0], y, s.rows, s.F)) return GF_ERR_CUDA;
-    return pg::launch<pg::EPI_GATE>(cg, p, st, launches);
+    bool wide;
+    const int cg = gl::forward_cg(s, n_sm, &wide);
+    if (!gl::products(p, cg, wide, s, x, w, x2, w2) || !pg::out_map(&p.out[0], y, s.rows, s.F)) return GF_ERR_CUDA;
+    return pg::launch<pg::EPI_GATE>(cg, p, st, launches, wide);
 }
 
 // Workspace of the gradient: da and, where there is a second product, db, [rows][F] bf16 each.
@@ -96,9 +111,10 @@ inline gf_status_t gated_linear_backward(const __nv_bfloat16* x, const __nv_bflo
         GemmParams p = {};
         p.act = act;
         p.dy = dy;
-        const int cg = forward_cg(s, n_sm);
-        if (!products(p, cg, s, x, w, x2, w2) || !out_map(&p.out[0], da, s.rows, s.F) || (gated && !out_map(&p.out[1], db, s.rows, s.F))) return GF_ERR_CUDA;
-        const gf_status_t e = launch<EPI_GATE_GRAD>(cg, p, st, launches);
+        bool wide;
+        const int cg = forward_cg(s, n_sm, &wide);
+        if (!products(p, cg, wide, s, x, w, x2, w2) || !out_map(&p.out[0], da, s.rows, s.F) || (gated && !out_map(&p.out[1], db, s.rows, s.F))) return GF_ERR_CUDA;
+        const gf_status_t e = launch<EPI_GATE_GRAD>(cg, p, st, launches, wide);
         if (e != GF_OK) return e;
     }
     GemmParams p = {};

@@ -13,7 +13,10 @@
 //
 // A tile's columns can be shared out in halves (B_DUAL, B_HALF): the left half holds columns of a first product, the right half the
 // same columns of a second one, so that an epilogue sees both values of an element (the gated linear block).  B_DUAL: both
-// products have the same A and run as one; B_HALF: each has its own A and depth, and they run one after the other.
+// products have the same A and run as one; B_HALF: each has its own A and depth, and they run one after the other.  As products of half a
+// tile's columns keep the tensor cores at 3/4 of their rate (an instruction reads as much of A for half the work), WIDE gives each of two
+// deep products a whole 256 x 256 accumulator; these fill tensor memory, so there is one set, and what the epilogue can do with the
+// first product alone it does while the second one runs.
 //
 //   warp 0      TMA producer: 64 contraction indices of A and B (16 KB each per CTA) per stage of a six-stage ring
 //   warp 1      tensor-memory allocation; an elected lane of the leading CTA issues the four products of a stage
@@ -41,7 +44,7 @@ constexpr int OFF_SLAB = NSTAGE * STAGE_BYTES;        // [N_EPI warps][32 rows x
 constexpr int OFF_MISC = OFF_SLAB + N_EPI * 4096;     // abort word, wait limit, tensor-memory address, barriers
 constexpr int SMEM = OFF_MISC + 256 + 1024;           // + slack for manual 1024-byte alignment
 static_assert(SMEM <= 232448, "shared memory budget of one sm_100 CTA");
-enum { BAR_FULL = 0, BAR_EMPTY = NSTAGE, BAR_ACC_FULL = 2 * NSTAGE, BAR_ACC_EMPTY = BAR_ACC_FULL + 2, BAR_DRAIN = BAR_ACC_EMPTY + 2, N_BARS };
+enum { BAR_FULL = 0, BAR_EMPTY = NSTAGE, BAR_ACC_FULL = 2 * NSTAGE, BAR_ACC_EMPTY = BAR_ACC_FULL + 2, BAR_LEFT_FULL = BAR_ACC_EMPTY + 2, BAR_DRAIN, N_BARS };
 static_assert(16 + 8 * N_BARS <= 256, "barrier block");
 
 // what the epilogue makes of an accumulator
@@ -221,12 +224,35 @@ __device__ __forceinline__ void tile_at(const GemmParams& p, int tile, int& gi, 
     tm = 8 * band + rest - tn * h;
 }
 
-template <int CG, Epilogue EPI>
+__device__ __forceinline__ void st_acc(uint32_t taddr, const float (&o)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};\n\t"
+        "tcgen05.wait::st.sync.aligned;"
+        ::"r"(taddr), "f"(o[0]), "f"(o[1]), "f"(o[2]), "f"(o[3]), "f"(o[4]), "f"(o[5]), "f"(o[6]), "f"(o[7]), "f"(o[8]), "f"(o[9]), "f"(o[10]), "f"(o[11]),
+          "f"(o[12]), "f"(o[13]), "f"(o[14]), "f"(o[15]), "f"(o[16]), "f"(o[17]), "f"(o[18]), "f"(o[19]), "f"(o[20]), "f"(o[21]), "f"(o[22]), "f"(o[23]),
+          "f"(o[24]), "f"(o[25]), "f"(o[26]), "f"(o[27]), "f"(o[28]), "f"(o[29]), "f"(o[30]), "f"(o[31])
+        : "memory");
+}
+// 32 bf16 values of a row that has `left` more of them (a multiple of 8); zeros past its end and where the row is none
+__device__ __forceinline__ void load_row32(const __nv_bfloat16* src, bool in, int left, uint32_t (&d)[16])
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint4 u = in && 8 * q < left ? __ldg(reinterpret_cast<const uint4*>(src) + q) : make_uint4(0u, 0u, 0u, 0u);
+        d[4 * q] = u.x; d[4 * q + 1] = u.y; d[4 * q + 2] = u.z; d[4 * q + 3] = u.w;
+    }
+}
+__device__ __forceinline__ float bf16_at(const uint32_t (&d)[16], int j) { return __uint_as_float(j & 1 ? d[j / 2] & 0xffff0000u : d[j / 2] << 16); }
+
+template <int CG, Epilogue EPI, bool WIDE>
 __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_constant__ GemmParams p)
 {
     constexpr int BN = 128 * CG;                      // columns of a tile
-    constexpr int HW = BN / 2;
-    constexpr int ACC_COLS = 256;                     // two accumulator sets
+    constexpr int HW = WIDE ? BN : BN / 2;            // columns of a half
+    constexpr int SETS = WIDE ? 1 : 2, ACC_COLS = 256;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t sbase = smem_u32(smem);
@@ -247,6 +273,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
             mbar_init(bar(BAR_ACC_FULL + i), 1);
             mbar_init(bar(BAR_ACC_EMPTY + i), N_EPI * CG);
         }
+        mbar_init(bar(BAR_LEFT_FULL), 1);
         mbar_init(bar(BAR_DRAIN), 1);
         sts32(abort_flag, 0u);
         sts32(abort_flag + 4, ck::WAIT_LIMIT_US);
@@ -320,7 +347,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                 int gi, tm, tn;
                 tile_at(p, tile, gi, tm, tn);
                 const Group& g = p.g[gi];
-                const int set = ti & 1, use = ti >> 1;
+                const int set = SETS == 2 ? ti & 1 : 0, use = SETS == 2 ? ti >> 1 : ti;
                 // the epilogue has read this set's previous tile out of tensor memory
                 if (use >= 1 && !mbar_wait_warp(bar(BAR_ACC_EMPTY + set), (use + 1) & 1, abort_flag)) { alive = false; break; }
                 tc_fence_after();
@@ -341,9 +368,10 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                                 if constexpr (CG == 2) tc_mma_pair(acc, da + a_step * kk, db + b_step * kk, idesc, on);
                                 else tc_mma(acc, da + a_step * kk, db + b_step * kk, idesc, on);
                             }
-                            const bool last = ks == sg.steps - 1 && q == g.n_seg - 1;
+                            const bool last = ks == sg.steps - 1 && q == g.n_seg - 1, left = WIDE && ks == sg.steps - 1 && q == 0;
                             if constexpr (CG == 2) {
                                 tc_commit_pair(bar(BAR_EMPTY + s));
+                                if (left) tc_commit_pair(bar(BAR_LEFT_FULL));
                                 if (last) tc_commit_pair(bar(BAR_ACC_FULL + set));
                             } else {
                                 tc_commit(bar(BAR_EMPTY + s));
@@ -374,8 +402,8 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
             int gi, tm, tn;
             tile_at(p, tile, gi, tm, tn);
             const Group& g = p.g[gi];
-            const int set = ti & 1;
-            if (!mbar_wait_warp(bar(BAR_ACC_FULL + set), (ti >> 1) & 1, abort_flag)) break;
+            const int set = SETS == 2 ? ti & 1 : 0;
+            if (!mbar_wait_warp(bar(WIDE ? BAR_LEFT_FULL : BAR_ACC_FULL + set), (SETS == 2 ? ti >> 1 : ti) & 1, abort_flag)) break;
             tc_fence_after();
             const uint32_t acc = tmem + ((uint32_t)(32 * sp) << 16) + ACC_COLS * set;
             const int row0 = tm * 128 * CG + 128 * (int)rank + 32 * sp, row = row0 + lane;
@@ -434,6 +462,79 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                         send(&p.out[g.out], col);
                     }
                 }
+            } else if constexpr (EPI == EPI_GATE && WIDE) {
+                // the activation goes back where its argument was while the second product runs
+                for (int c = 64 * part; c < HW && tn * HW + c < g.cols; c += 128)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        float a[32];
+                        ld_acc(acc + c + 32 * half, a);
+                        by_act(p.act, [&](auto k) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) a[j] = act_value<decltype(k)::value>(a[j]);
+                        });
+                        st_acc(acc + c + 32 * half, a);
+                    }
+                if (!mbar_wait_warp(bar(BAR_ACC_FULL), ti & 1, abort_flag)) break;
+                tc_fence_after();
+                for (int c = 64 * part; c < HW; c += 128) {
+                    const int col = tn * HW + c;
+                    if (col >= g.cols) break;
+                    take_slab();
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        float a[32], b[32];
+                        ld_acc(acc + c + 32 * half, a);
+                        ld_acc(acc + HW + c + 32 * half, b);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) a[j] *= b[j];
+                        put_bf16(sl, lane, half, a);
+                    }
+                    send(&p.out[0], col);
+                }
+            } else if constexpr (EPI == EPI_GATE_GRAD && WIDE) {
+                // db needs the first product alone: it leaves, and dy act'(a) takes the first product's place, while the second one runs
+                for (int c = 64 * part; c < HW; c += 128) {
+                    const int col = tn * HW + c;
+                    if (col >= g.cols) break;
+                    take_slab();
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        uint32_t d[16];
+                        load_row32(p.dy + (size_t)row * g.cols + col + 32 * half, in, g.cols - col - 32 * half, d);
+                        float a[32], b[32];
+                        ld_acc(acc + c + 32 * half, a);
+                        by_act(p.act, [&](auto k) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) {
+                                float f, df;
+                                act_grad<decltype(k)::value>(a[j], f, df);
+                                a[j] = bf16_at(d, j) * df;
+                                b[j] = bf16_at(d, j) * f;
+                            }
+                        });
+                        st_acc(acc + c + 32 * half, a);
+                        put_bf16(sl, lane, half, b);
+                    }
+                    send(&p.out[1], col);
+                }
+                if (!mbar_wait_warp(bar(BAR_ACC_FULL), ti & 1, abort_flag)) break;
+                tc_fence_after();
+                for (int c = 64 * part; c < HW; c += 128) {
+                    const int col = tn * HW + c;
+                    if (col >= g.cols) break;
+                    take_slab();
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        float a[32], b[32];
+                        ld_acc(acc + c + 32 * half, a);
+                        ld_acc(acc + HW + c + 32 * half, b);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) a[j] *= b[j];
+                        put_bf16(sl, lane, half, a);
+                    }
+                    send(&p.out[0], col);
+                }
             } else if constexpr (EPI == EPI_GATE) {
                 const int width = p.gated ? HW : BN;
                 for (int c = 64 * part; c < width; c += 128) {
@@ -468,13 +569,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         uint32_t d[16];
-                        const __nv_bfloat16* src = p.dy + (size_t)row * g.cols + col + 32 * half;
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const uint4 u = in && col + 32 * half + 8 * q < g.cols ? __ldg(reinterpret_cast<const uint4*>(src) + q) : make_uint4(0u, 0u, 0u, 0u);
-                            d[4 * q] = u.x; d[4 * q + 1] = u.y; d[4 * q + 2] = u.z; d[4 * q + 3] = u.w;
-                        }
-                        auto dy = [&](int j) { return __uint_as_float(j & 1 ? d[j / 2] & 0xffff0000u : d[j / 2] << 16); };
+                        load_row32(p.dy + (size_t)row * g.cols + col + 32 * half, in, g.cols - col - 32 * half, d);
                         float a[32];
                         ld_acc(acc + c + 32 * half, a);
                         if (p.gated) {
@@ -485,8 +580,8 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                                 for (int j = 0; j < 32; ++j) {
                                     float f, df;
                                     act_grad<decltype(k)::value>(a[j], f, df);
-                                    a[j] = dy(j) * b[j] * df;
-                                    b[j] = dy(j) * f;
+                                    a[j] = bf16_at(d, j) * b[j] * df;
+                                    b[j] = bf16_at(d, j) * f;
                                 }
                             });
 #pragma unroll
@@ -497,7 +592,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                                 for (int j = 0; j < 32; ++j) {
                                     float f, df;
                                     act_grad<decltype(k)::value>(a[j], f, df);
-                                    a[j] = dy(j) * df;
+                                    a[j] = bf16_at(d, j) * df;
                                 }
                             });
                         }
@@ -634,25 +729,28 @@ inline void add_group(GemmParams& p, const Group& g)
     ++p.n_groups;
 }
 
-template <int CG, Epilogue EPI>
+template <int CG, Epilogue EPI, bool WIDE>
 inline cudaError_t launch_one(const GemmParams& p, int n_sm, int dev, cudaStream_t st)
 {
     static PerDeviceFlag attr_set;
     if (!attr_set.is_set(dev)) {
-        const cudaError_t e = cudaFuncSetAttribute(pair_gemm_kernel<CG, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+        const cudaError_t e = cudaFuncSetAttribute(pair_gemm_kernel<CG, EPI, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
         if (e != cudaSuccess) return e;
         attr_set.set(dev);
     }
     const int units = n_sm / CG;
     const unsigned grid = (unsigned)(CG * (p.n_tiles < units ? p.n_tiles : units));
-    return launch_pdl_cluster(pair_gemm_kernel<CG, EPI>, grid, THREADS, SMEM, CG, st, p);
+    return launch_pdl_cluster(pair_gemm_kernel<CG, EPI, WIDE>, grid, THREADS, SMEM, CG, st, p);
 }
 template <Epilogue EPI>
-inline gf_status_t launch(int cg, const GemmParams& p, cudaStream_t st, std::atomic<uint64_t>* launches)
+inline gf_status_t launch(int cg, const GemmParams& p, cudaStream_t st, std::atomic<uint64_t>* launches, bool wide = false)
 {
     const int n_sm = sm_count(), dev = current_device();
     if (n_sm < 2 || dev < 0) return GF_ERR_CUDA;
-    const cudaError_t e = cg == 2 ? launch_one<2, EPI>(p, n_sm, dev, st) : launch_one<1, EPI>(p, n_sm, dev, st);
+    cudaError_t e = cudaErrorInvalidValue;
+    if (!wide) e = cg == 2 ? launch_one<2, EPI, false>(p, n_sm, dev, st) : launch_one<1, EPI, false>(p, n_sm, dev, st);
+    if constexpr (EPI == EPI_GATE || EPI == EPI_GATE_GRAD)
+        if (wide) e = launch_one<2, EPI, true>(p, n_sm, dev, st);
     launches->fetch_add(1, std::memory_order_relaxed);
     return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
 }

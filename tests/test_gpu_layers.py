@@ -185,7 +185,7 @@ def check_gate_grad(x, w, x2, w2, act, dy, got, what):
 
 # one row to several tiles; depths and widths on both sides of 64, 128, 256; single CTAs, clusters, pairs of CTAs (the large ones)
 GATES = [(1, 64, -1, 64), (1, 2048, 0, 200), (3, 72, 136, 8), (7, 8, 8, 8), (64, 128, 0, 64), (65, 136, -1, 136), (127, 64, 200, 72), (128, 256, 0, 128),
-         (129, 200, 328, 264), (333, 768, 0, 328), (600, 72, -1, 2056), (2500, 136, 200, 4008), (2305, 72, 0, 4104), (4096, 64, -1, 2560)]
+         (129, 200, 328, 264), (333, 768, 0, 328), (600, 72, -1, 2056), (2500, 136, 200, 4008), (2305, 72, 0, 4104), (1900, 264, 328, 2304), (4096, 64, -1, 2560)]
 
 
 @pytest.mark.parametrize("rows,K1,K2,F", GATES)
