@@ -481,15 +481,16 @@ GF_API gf_status_t gf_gated_linear(const void *x, const void *w, const void *x2,
  *   x, w, x2, w2, act, sizes   as for gf_gated_linear;   dy  DEVICE bf16 [rows][F]
  *   dx [rows][K1], dw [K1][F], dx2 [rows][K2], dw2 [K2][F]   DEVICE bf16, written; dw2 is NULL without w2, dx2 without x2; none may
  *                 be an input or another output
- *   workspace     DEVICE, gf_gated_linear_backward_workspace_bytes(rows,F,w2 != NULL) bytes, 16-byte aligned (da and db);
- *                 GF_ERR_WORKSPACE if absent or too small
+ *   workspace     DEVICE, gf_gated_linear_backward_workspace_bytes(rows,K1,K2,F,same) bytes, 16-byte aligned, with K2 = 0 without w2 and
+ *                 same = 1 where x2 is NULL for x (da and db, and fp32 sums of products that are cut along their
+ *                 contraction index, on the current device); GF_ERR_WORKSPACE if absent or too small
  * relu^2 has derivative 0 at 0.  da and db are rounded to bf16 (they are operands of the second products), sums are fp32, results
- * rounded once; no atomics.  rows = 0 writes zeros to dw and dw2.  Enqueues two kernels on `stream`, allocates nothing, does not
- * synchronise. */
+ * rounded once, in an order that the sizes and the GPU alone decide.  rows = 0 writes zeros to dw and dw2.  Enqueues two kernels on
+ * `stream` (three where a product is cut), allocates nothing, does not synchronise. */
 GF_API gf_status_t gf_gated_linear_backward(const void *x, const void *w, const void *x2, const void *w2, int act,
                                      const void *dy, void *dx, void *dw, void *dx2, void *dw2, long long rows, int K1,
                                      int K2, int F, void *workspace, size_t workspace_bytes, gf_stream_t stream);
-GF_API size_t gf_gated_linear_backward_workspace_bytes(long long rows, int F, int gated);
+GF_API size_t gf_gated_linear_backward_workspace_bytes(long long rows, int K1, int K2, int F, int same);
 
 /* Cross entropy of a linear layer over the vocabulary, without keeping the logits.  For every row
  *     z = x W^T,   lse = log sum_v exp(z[v]),   loss = lse - z[target].
@@ -510,9 +511,11 @@ GF_API size_t gf_vocab_loss_workspace_bytes(long long rows, long long V);
  *   x, w, targets, sizes   as for gf_vocab_loss, lse what it wrote;   dloss  DEVICE fp32 [rows], or NULL for 1 in every row
  *   dx [rows][D], dw [V][D]   DEVICE bf16, written; neither may be an input
  *   workspace  DEVICE, gf_vocab_loss_backward_workspace_bytes(rows,D,V) bytes, 16-byte aligned; GF_ERR_WORKSPACE if absent or
- *              too small (256 MB for a piece of P, 2 KB per row at least; fp32 sums of dx where the vocabulary takes several pieces)
- * P is rounded to bf16 (it is an operand of both products), sums are fp32, results rounded once; no atomics.  rows = 0 writes zeros to
- * dw.  Enqueues two kernels per piece of the vocabulary on `stream`, allocates nothing, does not synchronise. */
+ *              too small (256 MB for a piece of P, 2 KB per row at least; fp32 sums of dx where the vocabulary takes several pieces, and of
+ *              products that are cut along their contraction index, 256 MB at most)
+ * P is rounded to bf16 (it is an operand of both products), sums are fp32, results rounded once, in an order that the sizes and the GPU
+ * alone decide.  rows = 0 writes zeros to dw.  Enqueues two kernels per piece of the vocabulary on `stream` (three where a product is
+ * cut), allocates nothing, does not synchronise. */
 GF_API gf_status_t gf_vocab_loss_backward(const void *x, const void *w, const int64_t *targets, const float *lse,
                                    const float *dloss, void *dx, void *dw, long long rows, int D, long long V,
                                    void *workspace, size_t workspace_bytes, gf_stream_t stream);

