@@ -263,6 +263,19 @@ __device__ __forceinline__ void load_row32(const __nv_bfloat16* src, bool in, in
         d[4 * q] = u.x; d[4 * q + 1] = u.y; d[4 * q + 2] = u.z; d[4 * q + 3] = u.w;
     }
 }
+// bit i where 0 <= i < 32, else nothing
+__device__ __forceinline__ uint32_t one_of_32(long long i) { return i >= 0 && i < 32 ? 1u << (int)i : 0u; }
+// v <- exp(v - r); the difference first: of logits far from zero it is exact where it matters
+__device__ __forceinline__ void exp_of_difference(float (&v)[32], float r)
+{
+    const float2 neg = make_float2(-r, -r), l2e = make_float2(LOG2E, LOG2E);
+#pragma unroll
+    for (int j = 0; j < 32; j += 2) {
+        const float2 d = mul2(add2(make_float2(v[j], v[j + 1]), neg), l2e);
+        v[j] = ex2(d.x);
+        v[j + 1] = ex2(d.y);
+    }
+}
 __device__ __forceinline__ float bf16_at(const uint32_t (&d)[16], int j) { return __uint_as_float(j & 1 ? d[j / 2] & 0xffff0000u : d[j / 2] << 16); }
 
 template <int CG, Epilogue EPI, bool WIDE>
@@ -422,12 +435,37 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
             const Tile place = tile_at(p, tile);
             const Group& g = p.g[place.g];
             const int tm = place.m, tn = place.n;
+            const int row0 = tm * 128 * CG + 128 * (int)rank + 32 * sp, row = row0 + lane;
+            const bool in = row < g.rows;
+            // what the epilogue reads from memory is under way while the products run
+            const int width = EPI == EPI_GATE || EPI == EPI_GATE_GRAD ? (WIDE || p.gated ? HW : BN) : BN;
+            constexpr int DY_BLOCKS = EPI == EPI_GATE_GRAD ? (BN + 127) / 128 : 1;      // blocks of 64 columns that a warp takes
+            uint32_t dy[DY_BLOCKS][2][16];
+            if constexpr (EPI == EPI_GATE_GRAD) {
+#pragma unroll
+                for (int k = 0; k < DY_BLOCKS; ++k)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const int c = 64 * part + 128 * k + 32 * half, col = tn * width + c;
+                        load_row32(p.dy + (size_t)row * g.cols + col, in && c < width, g.cols - col, dy[k][half]);
+                    }
+            }
+            long long target = -1;                    // (-1: none)
+            float lse = 0.f, weight = 0.f;
+            if constexpr (EPI == EPI_LSE || EPI == EPI_PROB) {
+                if (in) target = p.targets[row];
+                if (target < 0 || target >= p.vocab) target = -1;
+            }
+            if constexpr (EPI == EPI_PROB) {
+                if (in) {
+                    lse = p.lse[row];
+                    weight = target < 0 ? 0.f : p.dloss ? p.dloss[row] : 1.f;
+                }
+            }
             const int set = SETS == 2 ? ti & 1 : 0;
             if (!mbar_wait_warp(bar(WIDE ? BAR_LEFT_FULL : BAR_ACC_FULL + set), (SETS == 2 ? ti >> 1 : ti) & 1, abort_flag)) break;
             tc_fence_after();
             const uint32_t acc = tmem + ((uint32_t)(32 * sp) << 16) + ACC_COLS * set;
-            const int row0 = tm * 128 * CG + 128 * (int)rank + 32 * sp, row = row0 + lane;
-            const bool in = row < g.rows;
             // the slab, once no store is reading it any more
             auto take_slab = [&]() {
                 if (lane == 0) bulk_wait_read<0>();
@@ -514,14 +552,14 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                 }
             } else if constexpr (EPI == EPI_GATE_GRAD && WIDE) {
                 // db needs the first product alone: it leaves, and dy act'(a) takes the first product's place, while the second one runs
-                for (int c = 64 * part; c < HW; c += 128) {
-                    const int col = tn * HW + c;
+#pragma unroll
+                for (int k = 0; k < DY_BLOCKS; ++k) {
+                    const int c = 64 * part + 128 * k, col = tn * HW + c;
                     if (col >= g.cols) break;
                     take_slab();
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        uint32_t d[16];
-                        load_row32(p.dy + (size_t)row * g.cols + col + 32 * half, in, g.cols - col - 32 * half, d);
+                        const uint32_t(&d)[16] = dy[k][half];
                         float a[32], b[32];
                         ld_acc(acc + c + 32 * half, a);
                         by_act(p.act, [&](auto k) {
@@ -556,7 +594,6 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                     send(&p.out[0], col);
                 }
             } else if constexpr (EPI == EPI_GATE) {
-                const int width = p.gated ? HW : BN;
                 for (int c = 64 * part; c < width; c += 128) {
                     const int col = tn * width + c;
                     if (col >= g.cols) break;
@@ -580,16 +617,15 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                     send(&p.out[0], col);
                 }
             } else if constexpr (EPI == EPI_GATE_GRAD) {
-                const int width = p.gated ? HW : BN;
-                for (int c = 64 * part; c < width; c += 128) {
-                    const int col = tn * width + c;
-                    if (col >= g.cols) break;
+#pragma unroll
+                for (int k = 0; k < DY_BLOCKS; ++k) {
+                    const int c = 64 * part + 128 * k, col = tn * width + c;
+                    if (c >= width || col >= g.cols) break;
                     take_slab();
                     uint32_t later[2][16];            // db, in bf16, until da has left the slab
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        uint32_t d[16];
-                        load_row32(p.dy + (size_t)row * g.cols + col + 32 * half, in, g.cols - col - 32 * half, d);
+                        const uint32_t(&d)[16] = dy[k][half];
                         float a[32];
                         ld_acc(acc + c + 32 * half, a);
                         if (p.gated) {
@@ -631,7 +667,6 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                 // a warp takes half of the tile's columns.  exp is taken of differences to a reference, the largest value so far (0
                 // instead of an infinite one: the sum is then infinite, or zero, by itself); a NaN reaches the sum through its own exponential
                 float ref = -FLT_MAX, sum = 0.f;
-                const long long t = in ? p.targets[row] : -1;
                 for (int c = HW * part; c < HW * part + HW; c += 32) {
                     const int col = tn * BN + c;
                     if (col >= g.cols) break;
@@ -642,30 +677,29 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                         for (int j = 0; j < 32; ++j)
                             if (col + j >= g.cols) v[j] = -INFINITY;
                     }
-                    if (t >= col && t < col + 32 && t < g.cols) {
-                        float z = v[0];
+                    const uint32_t hit = one_of_32(target - col);
+                    if (__any_sync(0xffffffffu, hit)) {
+                        float z = 0.f;
 #pragma unroll
-                        for (int j = 1; j < 32; ++j) z = (int)t - col == j ? v[j] : z;
-                        p.target_logit[row] = z;
+                        for (int j = 0; j < 32; ++j) z = hit >> j & 1 ? v[j] : z;
+                        if (hit) p.target_logit[row] = z;
                     }
-                    float top = v[0];
+                    float t4[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-                    for (int j = 1; j < 32; ++j) top = fmaxf(top, v[j]);
+                    for (int j = 4; j < 32; ++j) t4[j & 3] = fmaxf(t4[j & 3], v[j]);
+                    float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
                     top = c == HW * part ? top : fmaxf(top, ref);
                     top = fabsf(top) < INFINITY ? top : 0.f;
-                    float s4[4] = {sum * ex2((ref - top) * LOG2E), 0.f, 0.f, 0.f};
+                    float2 s2[2] = {make_float2(sum * ex2((ref - top) * LOG2E), 0.f), make_float2(0.f, 0.f)};
+                    exp_of_difference(v, top);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) s4[j & 3] += ex2((v[j] - top) * LOG2E);
-                    sum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    for (int j = 0; j < 16; ++j) s2[j & 1] = add2(s2[j & 1], make_float2(v[2 * j], v[2 * j + 1]));
+                    sum = (s2[0].x + s2[0].y) + (s2[1].x + s2[1].y);
                     ref = top;
                 }
                 if (in) p.stats[(size_t)(2 * tn + part) * g.rows + row] = make_float2(ref, sum);
             } else {
-                const float lse = in ? p.lse[row] : 0.f;
-                long long t = in ? p.targets[row] : -1;
-                float w = t >= 0 && t < p.vocab ? 1.f : 0.f;
-                if (w != 0.f && p.dloss) w = p.dloss[row];
-                t = t >= 0 && t < p.vocab ? t - p.first_col : -1;
+                const long long at = target < 0 ? -1 : target - p.first_col;
                 for (int c = 64 * part; c < BN; c += 128) {
                     const int col = tn * BN + c;
                     if (col >= g.cols) break;
@@ -674,16 +708,18 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                     for (int half = 0; half < 2; ++half) {
                         float v[32];
                         ld_acc(acc + c + 32 * half, v);
+                        exp_of_difference(v, lse);
+                        const uint32_t hit = one_of_32(at - (col + 32 * half));
+                        if (__any_sync(0xffffffffu, hit)) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = ex2((v[j] - lse) * LOG2E);
-                        const long long at = t - (col + 32 * half);
-                        if (at >= 0 && at < 32) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if ((int)at == j) v[j] -= 1.f;
+                            for (int j = 0; j < 32; ++j) v[j] -= hit >> j & 1 ? 1.f : 0.f;
                         }
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] *= w;
+                        for (int j = 0; j < 32; j += 2) {
+                            const float2 o = mul2(make_float2(v[j], v[j + 1]), make_float2(weight, weight));
+                            v[j] = o.x;
+                            v[j + 1] = o.y;
+                        }
                         if (col + 32 * half + 32 > g.cols) {          // (columns that fill up a row of the tensor: an operand, so zero)
 #pragma unroll
                             for (int j = 0; j < 32; ++j)

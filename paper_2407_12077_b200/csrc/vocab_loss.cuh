@@ -16,16 +16,19 @@ namespace vl {
 using namespace pg;
 using gl::choose_cg;
 
-constexpr int JOIN_WARPS = 16;
+constexpr int JOIN_THREADS = 512;
 
-// stats [tiles][rows] -> lse, loss.  A block takes 32 rows, its warps every JOIN_WARPS-th tile.
-__global__ void __launch_bounds__(32 * JOIN_WARPS) join_kernel(const float2* __restrict__ stats, const float* __restrict__ target_logit,
-                                                               const long long* __restrict__ targets, long long vocab, int tiles, int rows,
-                                                               float* __restrict__ loss, float* __restrict__ lse)
+// stats [tiles][rows] -> lse, loss.  A block takes ROWS rows, JOIN_THREADS / ROWS threads sharing the tiles of each out between them: 32
+// rows read whole lines; a call with fewer has more threads on each (7 rows, 626 half tiles: 10 us with 32 rows to a block).
+template <int ROWS>
+__global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const float2* __restrict__ stats, const float* __restrict__ target_logit,
+                                                            const long long* __restrict__ targets, long long vocab, int tiles, int rows,
+                                                            float* __restrict__ loss, float* __restrict__ lse)
 {
-    __shared__ float2 part[JOIN_WARPS][32];
+    constexpr int SHARES = JOIN_THREADS / ROWS;
+    __shared__ float2 part[SHARES][ROWS];
     asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x * 32 + lane;
+    const int share = threadIdx.x / ROWS, r = threadIdx.x % ROWS, row = blockIdx.x * ROWS + r;
     float ref = -INFINITY, sum = 0.f;
     // (references are finite, so a first one's factor below is exp(-inf) = 0)
     auto join = [&](float2 o) {
@@ -34,20 +37,26 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) join_kernel(const float2* __r
         ref = top;
     };
     if (row < rows) {
-        int t = warp;
-        for (; t + 3 * JOIN_WARPS < tiles; t += 4 * JOIN_WARPS) {
+        int t = share;
+        for (; t + 3 * SHARES < tiles; t += 4 * SHARES) {
             float2 o[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) o[q] = stats[(size_t)(t + q * JOIN_WARPS) * rows + row];
+            for (int q = 0; q < 4; ++q) o[q] = stats[(size_t)(t + q * SHARES) * rows + row];
 #pragma unroll
             for (int q = 0; q < 4; ++q) join(o[q]);
         }
-        for (; t < tiles; t += JOIN_WARPS) join(stats[(size_t)t * rows + row]);
+        for (; t < tiles; t += SHARES) join(stats[(size_t)t * rows + row]);
     }
-    part[warp][lane] = make_float2(ref, sum);
-    __syncthreads();
-    if (warp == 0 && row < rows) {
-        for (int w = 1; w < JOIN_WARPS && w < tiles; ++w) join(part[w][lane]);
+    part[share][r] = make_float2(ref, sum);
+#pragma unroll
+    for (int h = SHARES / 2; h > 0; h /= 2) {         // (a share without tiles has -inf and joins nothing)
+        __syncthreads();
+        if (share < h && part[share + h][r].x > -INFINITY) {
+            join(part[share + h][r]);
+            part[share][r] = make_float2(ref, sum);
+        }
+    }
+    if (share == 0 && row < rows) {
         const float l = ref + logf(sum);
         const long long t = targets[row];
         lse[row] = l;
@@ -114,8 +123,10 @@ inline gf_status_t vocab_loss(const __nv_bfloat16* x, const __nv_bfloat16* w, co
     p.target_logit = reinterpret_cast<float*>(static_cast<char*>(ws) + vocab_stats_bytes(rows, V));
     const gf_status_t s = launch<EPI_LSE>(cg, p, st, launches);
     if (s != GF_OK) return s;
-    const cudaError_t e = launch_pdl(join_kernel, (unsigned)ceil_div(rows, 32), 32 * JOIN_WARPS, 0, st, p.stats, p.target_logit, targets, V, 2 * g.tiles_n,
-                                     (int)rows, loss, lse);
+    auto join = rows >= 1024 ? join_kernel<32> : rows >= 256 ? join_kernel<8> : join_kernel<1>;
+    const int block_rows = rows >= 1024 ? 32 : rows >= 256 ? 8 : 1;
+    const cudaError_t e = launch_pdl(join, (unsigned)ceil_div(rows, block_rows), JOIN_THREADS, 0, st, (const float2*)p.stats, (const float*)p.target_logit, targets, V,
+                                     2 * g.tiles_n, (int)rows, loss, lse);
     launches->fetch_add(1, std::memory_order_relaxed);
     return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
 }
