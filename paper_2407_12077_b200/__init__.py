@@ -32,7 +32,9 @@ _lib = None
 _native = None               # the binding's C++ part (csrc/binding.cpp), once the library is loaded and if it could be built
 _NATIVE_FNS = ("gf_wkv6_prefill", "gf_wkv6_prefill_f32", "gf_wkv6_prefill_c2", "gf_wkv6_prefill_varlen", "gf_wkv6_prefill_varlen_f32",
                "gf_wkv6_prefill_varlen_c2", "gf_wkv6_step", "gf_wkv6_step_f32", "gf_wkv6_step_c2", "gf_c2_layernorm", "gf_c2_layernorm_f32",
-               "gf_gold_key_compress", "gf_wkv6_workspace_bytes")
+               "gf_gold_key_compress", "gf_wkv6_workspace_bytes", "gf_c2_layernorm_backward", "gf_c2_layernorm_backward_f32",
+               "gf_c2_layernorm_backward_workspace_bytes", "gf_gated_linear", "gf_gated_linear_backward", "gf_gated_linear_backward_workspace_bytes",
+               "gf_vocab_loss", "gf_vocab_loss_workspace_bytes", "gf_vocab_loss_backward", "gf_vocab_loss_backward_workspace_bytes")
 _vp, _i, _sz, _ll = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_longlong
 
 # name -> (restype, argtypes); the single place the ABI is mirrored in Python
@@ -657,6 +659,12 @@ def layernorm_heads_backward(y, dout, gamma=None, eps=1e-5, want_params=True, dy
     latter two fp32 [H*N] (None unless want_params).  dy defaults to a new tensor (y or dout: in place); the workspace, unless a
     uint8 tensor of enough bytes is passed, is allocated here."""
     lib = _lib or load_library()
+    if _native is not None and stream is None and want_params and dy is None and workspace is None:
+        res = _native.layernorm_backward(y, dout, gamma, eps)
+        if res is not None:
+            if type(res) is int:
+                _check(res, "gf_c2_layernorm_backward" + _suffix(y.dtype))
+            return res
     H, N = y.shape[-2:]
     D = H * N
     rows = y.numel() // D if D else 0
@@ -707,6 +715,12 @@ def gated_linear(x, w, x2=None, w2=None, act="silu", out=None, stream=None):
     x: [..., K1], x2: [..., K2], w: [K1, F], w2: [K2, F], all bf16 contiguous CUDA tensors; act: "sigmoid", "relu2", "silu" or
     "gelu".  Returns [..., F] bf16 (allocated here unless passed as out)."""
     lib = _lib or load_library()
+    if _native is not None and stream is None and out is None:
+        res = _native.gated_linear(x, w, x2, w2, ACTIVATIONS.get(act))
+        if res is not None:
+            if type(res) is int:
+                _check(res, "gf_gated_linear")
+            return res
     ptrs, code, (rows, K1, K2, F) = _gated_args(x, w, x2, w2, act)
     _one_device(x=x, w=w, x2=x2, w2=w2, out=out)
     shape = tuple(x.shape[:-1]) + (F,)
@@ -722,6 +736,12 @@ def gated_linear_backward(x, w, dy, x2=None, w2=None, act="silu", stream=None, w
     bf16; dx2 is None without x2 (dx then has both products' parts), dw2 without w2.  The workspace, unless a uint8 tensor of
     enough bytes is passed, is allocated here."""
     lib = _lib or load_library()
+    if _native is not None and stream is None and workspace is None:
+        res = _native.gated_linear_backward(x, w, dy, x2, w2, ACTIVATIONS.get(act))
+        if res is not None:
+            if type(res) is int:
+                _check(res, "gf_gated_linear_backward")
+            return res
     ptrs, code, (rows, K1, K2, F) = _gated_args(x, w, x2, w2, act)
     _one_device(x=x, w=w, x2=x2, w2=w2, dy=dy, workspace=workspace)
     outs = [None if t is None else torch.empty_like(t) for t in (x, w, x2, w2)]
@@ -750,6 +770,12 @@ def vocab_loss(x, w, targets, stream=None, workspace=None):
     fp32 [...]; lse is what vocab_loss_backward() takes.  The workspace, unless a uint8 tensor of enough bytes is passed, is
     allocated here."""
     lib = _lib or load_library()
+    if _native is not None and stream is None and workspace is None:
+        res = _native.vocab_loss(x, w, targets)
+        if res is not None:
+            if type(res) is int:
+                _check(res, "gf_vocab_loss")
+            return res
     ptrs, (rows, D, V), shape = _vocab_args(x, w, targets)
     _one_device(x=x, w=w, targets=targets, workspace=workspace)
     loss, lse = (torch.empty(shape, device=x.device, dtype=torch.float32) for _ in range(2))
@@ -764,6 +790,12 @@ def vocab_loss_backward(x, w, targets, lse, dloss=None, stream=None, workspace=N
     """gf_vocab_loss_backward: gradient of sum(dloss * loss) for vocab_loss(x, w, targets), whose lse it takes; dloss: fp32 [...]
     or None (ones).  Returns (dx, dw) in bf16.  The workspace, unless a uint8 tensor of enough bytes is passed, is allocated here."""
     lib = _lib or load_library()
+    if _native is not None and stream is None and workspace is None:
+        res = _native.vocab_loss_backward(x, w, targets, lse, dloss)
+        if res is not None:
+            if type(res) is int:
+                _check(res, "gf_vocab_loss_backward")
+            return res
     ptrs, (rows, D, V), shape = _vocab_args(x, w, targets)
     _one_device(x=x, w=w, targets=targets, lse=lse, dloss=dloss, workspace=workspace)
     dx, dw = torch.empty_like(x), torch.empty_like(w)

@@ -295,6 +295,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
     const int unit = blockIdx.x / CG, units = gridDim.x / CG;
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (warp == 2 && lane < MAX_IN) asm volatile("prefetch.tensormap [%0];" ::"l"(&p.in[lane]) : "memory");      // (of the launch's parameters)
     if (tid == 0) {
         for (int i = 0; i < NSTAGE; ++i) {
             mbar_init(bar(BAR_FULL + i), 1);
@@ -868,8 +869,8 @@ inline long long plan_time(const Product* q, int n, int cg, const int* slices, i
         worst = t > worst ? t : worst;
     }
     worst += all;
-    // a step of a pair is 0.3 us: a further launch about 4 us, the sums' bytes at 6 TB/s
-    return worst + (sum_bytes ? 100 + sum_bytes / 220000 : 0);
+    // a step of a pair is 0.25 us: a further launch, with its set-up and its wait, about 5 us, the sums' bytes at 6 TB/s
+    return worst + (sum_bytes ? 150 + sum_bytes / 220000 : 0);
 }
 inline Plan plan_products(const Product* q, int n, int n_sm, bool kept)
 {
