@@ -21,47 +21,72 @@ struct Shape {
     bool same;                      // x2 is x
 };
 
-// Pairs of CTAs on 256 x 256 accumulators or single ones on 128 x 128 (see pair_gemm.cuh): `small` and `large` count the tiles.
+// Pairs of CTAs on 256 x 256 accumulators or single ones on 128 x 128 (see pair_gemm.cuh): `large` and `small` count the tiles.
 inline int choose_cg(long long large, long long small, int n_sm)
 {
     return ceil_div(large, n_sm / 2) * STEP_TIME[2] <= ceil_div(small, n_sm) * STEP_TIME[1] ? 2 : 1;
 }
 
+struct Launch {
+    int cg;
+    Mode mode;
+    int cluster;                    // SPLIT_TILES
+};
+
 // Both products of every column (maps 0: x, 1: w, 2: w2, 3: x2; all as they lie in memory, weights [K][F]).
-inline bool products(GemmParams& p, int cg, bool wide, const Shape& s, const __nv_bfloat16* x, const __nv_bfloat16* w, const __nv_bfloat16* x2, const __nv_bfloat16* w2)
+inline bool products(GemmParams& p, const Launch& l, const Shape& s, const __nv_bfloat16* x, const __nv_bfloat16* w, const __nv_bfloat16* x2, const __nv_bfloat16* w2)
 {
     const bool gated = s.K2 > 0;
     if (!in_map(&p.in[0], x, s.rows, s.K1) || !in_map(&p.in[1], w, s.K1, s.F)) return false;
     if (gated && (!in_map(&p.in[2], w2, s.K2, s.F) || !in_map(&p.in[3], x2, s.rows, s.K2))) return false;
-    Group g = make_group(cg, s.rows, s.F, gated && !wide ? 64 * cg : 128 * cg);
-    if (!gated || s.same) {
+    const bool whole = l.mode != TILES;               // an accumulator of a whole tile's columns for each product
+    Group g = make_group(l.cg, s.rows, s.F, gated && !whole ? 64 * l.cg : 128 * l.cg);
+    if (!gated || (s.same && !whole)) {
         add_segment(g, segment(0, false, 1, true, s.K1, gated ? B_DUAL : B_WHOLE));
     } else {
-        add_segment(g, segment(0, false, 1, true, s.K1, wide ? B_WHOLE : B_HALF, false));
-        add_segment(g, segment(3, false, 2, true, s.K2, wide ? B_WHOLE : B_HALF, true));
+        add_segment(g, segment(0, false, 1, true, s.K1, whole ? B_WHOLE : B_HALF, false));
+        add_segment(g, segment(3, false, 2, true, s.K2, whole ? B_WHOLE : B_HALF, true));
     }
     p.gated = gated;
     add_group(p, g);
     return true;
 }
-// The launch of both products: pairs of CTAs or single ones; *wide: a whole accumulator for each product (see pair_gemm.cuh).
-// Rounds of tiles times the time of one, in steps of a pair on 256 x 256: half tiles take 0.64 of one (16384 rows, 2048 and 7168 deep
-// -> 2048: 520 us, wide 408; 8192 rows, twice 512 -> 8192: 149, wide 126), a wide tile about two more for what its epilogue leaves
-// (8192 rows, twice 256 -> 8192: 103 and 101); where wide tiles are too few, half ones win (2048 rows, 768 and 2688 -> 768:
-// 20 us, wide 25).
-inline int forward_cg(const Shape& s, int n_sm, bool* wide)
+// How both products are launched: rounds of tiles times the time of one, in units of 1/30 us (STEP_TIME's).
+//  - Products of half a tile's columns take 0.64 of a whole tile's step (16384 rows, 2048 and 7168 deep -> 2048: 520 us, wide 408; 8192
+//    rows, twice 512 -> 8192: 149, wide 126), a wide tile about two steps more for what its epilogue leaves (8192 rows, twice 256
+//    -> 8192: 103 and 101); where wide tiles are too few, half ones win (2048 rows, 768 and 2688 -> 768: 20 us, wide 25).
+//  - A tile that a cluster divides costs the joining, 2 us.  Clusters must lie within one GPC, so not every SM finds a place in one:
+//    four fifths of them do (see key_compress.cuh).
+inline Launch forward_launch(const Shape& s, int n_sm, bool may_split)
 {
-    const long long m2 = ceil_div(s.rows, 256), m1 = ceil_div(s.rows, 128);
-    *wide = false;
+    const long long m2 = ceil_div(s.rows, 256), m1 = ceil_div(s.rows, 128), s1 = ceil_div(s.K1, 64), s2 = ceil_div(s.K2, 64), both = s1 + s2;
+    auto rounds = [&](long long tiles, int units) { return ceil_div(tiles, units); };
+    Launch best = {2, TILES, 2};
+    long long time;
+    auto offer = [&](int cg, Mode mode, int cluster, long long t) {
+        if (t < time) {
+            time = t;
+            best = Launch{cg, mode, cluster};
+        }
+    };
     if (s.K2 == 0 || s.same) {
         const int w = s.K2 > 0 ? 64 : 128;
-        return choose_cg(m2 * ceil_div(s.F, 2 * w), m1 * ceil_div(s.F, w), n_sm);
+        time = rounds(m2 * ceil_div(s.F, 2 * w), n_sm / 2) * s1 * STEP_TIME[2];
+        offer(1, TILES, 1, rounds(m1 * ceil_div(s.F, w), n_sm) * s1 * STEP_TIME[1]);
+    } else {
+        time = rounds(m2 * ceil_div(s.F, 256), n_sm / 2) * (both + 2) * STEP_TIME[2];
+        best.mode = WIDE_TILES;
+        offer(2, TILES, 2, rounds(m2 * ceil_div(s.F, 128), n_sm / 2) * both * 5);
+        offer(1, TILES, 1, rounds(m1 * ceil_div(s.F, 64), n_sm) * both * 6);
     }
-    const long long steps = ceil_div(s.K1, 64) + ceil_div(s.K2, 64);
-    const long long t_wide = ceil_div(m2 * ceil_div(s.F, 256), n_sm / 2) * (steps + 2) * 100;
-    const long long t_half = ceil_div(m2 * ceil_div(s.F, 128), n_sm / 2) * steps * 64, t_one = ceil_div(m1 * ceil_div(s.F, 64), n_sm) * steps * 45;
-    *wide = t_wide <= t_half && t_wide <= t_one;
-    return *wide || t_half <= t_one ? 2 : 1;
+    const long long tiles = m1 * ceil_div(s.F, 128);
+    if (may_split && tiles * 2 * 5 <= n_sm * 4LL) {
+        long long c = n_sm * 4 / (5 * tiles);
+        if (c > 8) c = 8;
+        if (c > both / 2) c = both / 2;               // two steps for each CTA
+        if (c >= 2) offer(1, SPLIT_TILES, (int)c, ceil_div(both, c) * STEP_TIME[1] + 60);
+    }
+    return best;
 }
 
 }  // namespace gl
@@ -73,10 +98,22 @@ inline gf_status_t gated_linear(const __nv_bfloat16* x, const __nv_bfloat16* w, 
     if (n_sm < 2) return GF_ERR_CUDA;
     pg::GemmParams p = {};
     p.act = act;
-    bool wide;
-    const int cg = gl::forward_cg(s, n_sm, &wide);
-    if (!gl::products(p, cg, wide, s, x, w, x2, w2) || !pg::out_map(&p.out[0], y, s.rows, s.F)) return GF_ERR_CUDA;
-    return pg::launch<pg::EPI_GATE>(cg, p, st, launches, wide);
+    const int dev = current_device();
+    if (dev < 0) return GF_ERR_CUDA;
+    p.y = y;
+    gl::Launch l = gl::forward_launch(s, n_sm, true);
+    if (!gl::products(p, l, s, x, w, x2, w2) || !pg::out_map(&p.out[0], y, s.rows, s.F)) return GF_ERR_CUDA;
+    if (l.mode == pg::SPLIT_TILES) {
+        if (pg::launch_one<1, pg::EPI_GATE, pg::SPLIT_TILES>(p, n_sm, dev, st, l.cluster) == cudaSuccess) {
+            launches->fetch_add(1, std::memory_order_relaxed);
+            return GF_OK;
+        }
+        cudaGetLastError();                           // (no cluster can be placed, on a partitioned device: whole tiles)
+        l = gl::forward_launch(s, n_sm, false);
+        p.n_groups = p.n_tiles = 0;
+        if (!gl::products(p, l, s, x, w, x2, w2)) return GF_ERR_CUDA;
+    }
+    return pg::launch<pg::EPI_GATE>(l.cg, p, st, launches, l.mode);
 }
 
 namespace gl {
@@ -117,10 +154,9 @@ inline gf_status_t gated_linear_backward(const __nv_bfloat16* x, const __nv_bflo
         GemmParams p = {};
         p.act = act;
         p.dy = dy;
-        bool wide;
-        const int cg = forward_cg(s, n_sm, &wide);
-        if (!products(p, cg, wide, s, x, w, x2, w2) || !out_map(&p.out[0], da, s.rows, s.F) || (gated && !out_map(&p.out[1], db, s.rows, s.F))) return GF_ERR_CUDA;
-        const gf_status_t e = launch<EPI_GATE_GRAD>(cg, p, st, launches, wide);
+        const Launch l = forward_launch(s, n_sm, false);
+        if (!products(p, l, s, x, w, x2, w2) || !out_map(&p.out[0], da, s.rows, s.F) || (gated && !out_map(&p.out[1], db, s.rows, s.F))) return GF_ERR_CUDA;
+        const gf_status_t e = launch<EPI_GATE_GRAD>(l.cg, p, st, launches, l.mode);
         if (e != GF_OK) return e;
     }
     GemmParams p = {};

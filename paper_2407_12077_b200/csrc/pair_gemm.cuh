@@ -16,7 +16,8 @@
 // products have the same A and run as one; B_HALF: each has its own A and depth, and they run one after the other.  As products of half a
 // tile's columns keep the tensor cores at 3/4 of their rate (an instruction reads as much of A for half the work), WIDE gives each of two
 // deep products a whole 256 x 256 accumulator; these fill tensor memory, so there is one set, and what the epilogue can do with the
-// first product alone it does while the second one runs.
+// first product alone it does while the second one runs.  SPLIT, for results of few tiles (decoding): a cluster of up to eight CTAs divides a tile's
+// contraction indices, leaves its sums in shared memory and adds them up there, each CTA a share of the tile's places.
 //
 //   warp 0      TMA producer: 64 contraction indices of A and B (16 KB each per CTA) per stage of a six-stage ring
 //   warp 1      tensor-memory allocation; an elected lane of the leading CTA issues the four products of a stage
@@ -42,6 +43,8 @@ constexpr int NSTAGE = 6;
 constexpr int STAGE_BYTES = 4 * TILE;                 // 128 x 64 of A, 128 x 64 of B
 constexpr int OFF_SLAB = NSTAGE * STAGE_BYTES;        // [N_EPI warps][32 rows x 128 B]
 constexpr int OFF_MISC = OFF_SLAB + N_EPI * 4096;     // abort word, wait limit, tensor-memory address, barriers
+constexpr int SUMS_PITCH = (2 * 128 + 4) * 4;          // SPLIT_TILES: a row of both products' sums, fp32, in place of the ring
+static_assert(128 * SUMS_PITCH <= OFF_SLAB, "partial sums");
 constexpr int SMEM = OFF_MISC + 256 + 1024;           // + slack for manual 1024-byte alignment
 static_assert(SMEM <= 232448, "shared memory budget of one sm_100 CTA");
 enum { BAR_FULL = 0, BAR_EMPTY = NSTAGE, BAR_ACC_FULL = 2 * NSTAGE, BAR_ACC_EMPTY = BAR_ACC_FULL + 2, BAR_LEFT_FULL = BAR_ACC_EMPTY + 2, BAR_DRAIN, N_BARS };
@@ -55,6 +58,7 @@ enum Epilogue {
     EPI_LSE,            // per row and tile of columns: maximum and sum of exponentials, and the target's logit
     EPI_PROB            // (exp(z - lse) - [column is the target]) * dloss
 };
+enum Mode { TILES, WIDE_TILES, SPLIT_TILES };
 enum BCols : unsigned char { B_WHOLE, B_DUAL, B_HALF };
 enum OutMode : unsigned char { OUT_BF16, OUT_F32, OUT_F32_ADD, OUT_BF16_ADD };   // (_ADD: onto, resp. with, the fp32 sums of earlier launches; F32: [slices][rows][cols])
 enum Act { ACT_SIGMOID = 0, ACT_RELU2 = 1, ACT_SILU = 2, ACT_GELU = 3 };
@@ -87,6 +91,7 @@ struct GemmParams {
     int act;
     bool gated;
     const __nv_bfloat16* dy;
+    __nv_bfloat16* y;               // SPLIT_TILES
     // EPI_LSE, EPI_PROB
     const long long* targets;
     long long vocab;                // a target outside [0, vocab) is none
@@ -222,7 +227,8 @@ struct Tile {
     int g, m, n;                    // group, place in it
     int slice, lo, hi;              // the steps it takes
 };
-__device__ __forceinline__ Tile tile_at(const GemmParams& p, int tile)
+// share, shares: of a tile that a cluster of CTAs divides (a group is cut into slices or divided, not both)
+__device__ __forceinline__ Tile tile_at(const GemmParams& p, int tile, int share, int shares)
 {
     Tile t;
     t.g = 0;
@@ -232,8 +238,9 @@ __device__ __forceinline__ Tile tile_at(const GemmParams& p, int tile)
     int i = tile - g.first;
     t.slice = i / places;
     i -= t.slice * places;
-    t.lo = (int)((long long)g.steps * t.slice / g.slices);
-    t.hi = (int)((long long)g.steps * (t.slice + 1) / g.slices);
+    const int of = g.slices * shares, nth = t.slice + share;
+    t.lo = (int)((long long)g.steps * nth / of);
+    t.hi = (int)((long long)g.steps * (nth + 1) / of);
     // bands of eight tiles along m, column by column: the tiles that run at one time share few rows of A and of B
     const int per = 8 * g.tiles_n, band = i / per, rest = i - band * per;
     const int h = min(8, g.tiles_m - 8 * band);
@@ -263,6 +270,8 @@ __device__ __forceinline__ void load_row32(const __nv_bfloat16* src, bool in, in
         d[4 * q] = u.x; d[4 * q + 1] = u.y; d[4 * q + 2] = u.z; d[4 * q + 3] = u.w;
     }
 }
+// blocks of 64 among `left` indices, at most the two of a CTA's operand
+__device__ __forceinline__ int tiles_of(int left) { return left <= 0 ? 0 : left <= 64 ? 1 : 2; }
 // bit i where 0 <= i < 32, else nothing
 __device__ __forceinline__ uint32_t one_of_32(long long i) { return i >= 0 && i < 32 ? 1u << (int)i : 0u; }
 // v <- exp(v - r); the difference first: of logits far from zero it is exact where it matters
@@ -278,12 +287,15 @@ __device__ __forceinline__ void exp_of_difference(float (&v)[32], float r)
 }
 __device__ __forceinline__ float bf16_at(const uint32_t (&d)[16], int j) { return __uint_as_float(j & 1 ? d[j / 2] & 0xffff0000u : d[j / 2] << 16); }
 
-template <int CG, Epilogue EPI, bool WIDE>
+template <int CG, Epilogue EPI, Mode MODE>
 __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_constant__ GemmParams p)
 {
     constexpr int BN = 128 * CG;                      // columns of a tile
-    constexpr int HW = WIDE ? BN : BN / 2;            // columns of a half
-    constexpr int SETS = WIDE ? 1 : 2, ACC_COLS = 256;
+    constexpr bool WIDE = MODE == WIDE_TILES, SPLIT = MODE == SPLIT_TILES;
+    static_assert(!WIDE || CG == 2, "pairs of CTAs");
+    static_assert(!SPLIT || (CG == 1 && EPI == EPI_GATE), "single CTAs, forward block");
+    constexpr int HW = MODE == TILES ? BN / 2 : BN;   // columns of a half
+    constexpr int SETS = MODE == TILES ? 2 : 1, ACC_COLS = 256;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t sbase = smem_u32(smem);
@@ -292,7 +304,12 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     uint32_t rank = 0;
     if constexpr (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    const int unit = blockIdx.x / CG, units = gridDim.x / CG;
+    uint32_t share = 0, shares = 1;                   // SPLIT: of a tile's contraction indices
+    if constexpr (SPLIT) {
+        asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(share));
+        asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(shares));
+    }
+    const int unit = blockIdx.x / (SPLIT ? shares : CG), units = gridDim.x / (SPLIT ? shares : CG);
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == 2 && lane < MAX_IN) asm volatile("prefetch.tensormap [%0];" ::"l"(&p.in[lane]) : "memory");      // (of the launch's parameters)
@@ -328,7 +345,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
         int s = 0, ph = 0, issued = 0;
         bool alive = true;
         for (int tile = unit; tile < p.n_tiles && alive; tile += units) {
-            const Tile t = tile_at(p, tile);
+            const Tile t = tile_at(p, tile, share, shares);
             const Group& g = p.g[t.g];
             const int m0 = t.m * 128 * CG + 128 * (int)rank, tn = t.n;
             for (int q = 0, at = 0; q < g.n_seg && alive; at += g.seg[q++].steps) {
@@ -337,6 +354,13 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                 // this CTA's columns of B: 128 of the tile's (one block of 64 where the tile's halves have products of their own)
                 const int n0 = sg.cols == B_WHOLE ? tn * BN + 128 * (int)rank : sg.cols == B_DUAL ? tn * HW : tn * HW + 64 * (int)rank;
                 const int n1 = sg.cols == B_DUAL && CG == 1 ? n0 : n0 + 64;
+                // tiles past the result's last row or column are not loaded: what multiplies them is not stored
+                const int a_here = tiles_of(g.rows - m0), b_here = sg.cols == B_DUAL && CG == 1 ? 2 : min(tiles_of(g.cols - n0), sg.cols == B_HALF ? 1 : 2);
+                int bytes = (a_here + b_here) * TILE;
+                if constexpr (CG == 2) {
+                    const int n_there = sg.cols == B_WHOLE ? n0 + 128 : sg.cols == B_DUAL ? n0 : n0 + 64;        // (of the other CTA; the leading one counts)
+                    bytes += (tiles_of(g.rows - m0 - 128) + min(tiles_of(g.cols - n_there), sg.cols == B_HALF ? 1 : 2)) * TILE;
+                }
                 const CUtensorMap* ma = &p.in[sg.a];
                 const CUtensorMap* mb0 = &p.in[sg.b + (sg.cols == B_DUAL && CG == 2 ? rank : 0)];
                 const CUtensorMap* mb1 = sg.cols == B_DUAL && CG == 1 ? &p.in[sg.b + 1] : mb0;
@@ -350,11 +374,11 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                             if constexpr (CG == 2) tma_load_pair(dst, m, c0, c1, full);
                             else tma_load_2d(dst, m, c0, c1, full);
                         };
-                        if (rank == 0) mbar_expect_tx(bar(BAR_FULL + s), (sg.cols == B_HALF ? 3 : 4) * TILE * CG);
-                        load(st, ma, sg.a_mn ? m0 : k, sg.a_mn ? k : m0);
-                        load(st + TILE, ma, sg.a_mn ? m0 + 64 : k, sg.a_mn ? k : m0 + 64);
-                        load(st + 2 * TILE, mb0, sg.b_mn ? n0 : k, sg.b_mn ? k : n0);
-                        if (sg.cols != B_HALF) load(st + 3 * TILE, mb1, sg.b_mn ? n1 : k, sg.b_mn ? k : n1);
+                        if (rank == 0) mbar_expect_tx(bar(BAR_FULL + s), bytes);
+                        if (a_here > 0) load(st, ma, sg.a_mn ? m0 : k, sg.a_mn ? k : m0);
+                        if (a_here > 1) load(st + TILE, ma, sg.a_mn ? m0 + 64 : k, sg.a_mn ? k : m0 + 64);
+                        if (b_here > 0) load(st + 2 * TILE, mb0, sg.b_mn ? n0 : k, sg.b_mn ? k : n0);
+                        if (b_here > 1) load(st + 3 * TILE, mb1, sg.b_mn ? n1 : k, sg.b_mn ? k : n1);
                     }
                     __syncwarp();
                     ++issued;
@@ -376,7 +400,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
             int s = 0, ph = 0, ti = 0;
             bool alive = true;
             for (int tile = unit; tile < p.n_tiles && alive; tile += units, ++ti) {
-                const Tile t = tile_at(p, tile);
+                const Tile t = tile_at(p, tile, share, shares);
                 const Group& g = p.g[t.g];
                 const int set = SETS == 2 ? ti & 1 : 0, use = SETS == 2 ? ti >> 1 : ti;
                 // the epilogue has read this set's previous tile out of tensor memory
@@ -433,7 +457,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
         const uint32_t sl = sbase + OFF_SLAB + (warp - 2) * 4096;
         int ti = 0;
         for (int tile = unit; tile < p.n_tiles; tile += units, ++ti) {
-            const Tile place = tile_at(p, tile);
+            const Tile place = tile_at(p, tile, share, shares);
             const Group& g = p.g[place.g];
             const int tm = place.m, tn = place.n;
             const int row0 = tm * 128 * CG + 128 * (int)rank + 32 * sp, row = row0 + lane;
@@ -519,6 +543,22 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                             put_bf16(sl, lane, half, v);
                         }
                         send(&p.out[g.out], col);
+                    }
+                }
+            } else if constexpr (SPLIT) {
+                // this CTA's sums to shared memory (the ring is free: every slice that was loaded has been multiplied)
+                for (int c = 64 * part; c < 2 * BN; c += 128) {
+                    if (c < BN ? place.lo >= g.seg[0].steps : place.hi <= g.seg[0].steps) continue;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        float v[32];
+                        ld_acc(acc + c + 32 * half, v);
+                        if (in) {
+#pragma unroll
+                            for (int q = 0; q < 8; ++q)
+                                sts128(sbase + (32 * sp + lane) * SUMS_PITCH + (c + 32 * half + 4 * q) * 4, __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]),
+                                       __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
+                        }
                     }
                 }
             } else if constexpr (EPI == EPI_GATE && WIDE) {
@@ -743,6 +783,43 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
     tc_fence_before();
     __syncthreads();
     if constexpr (CG == 2) cluster_sync();            // neither CTA's memory goes while the other's products or arrivals may reach it
+    if constexpr (SPLIT) {
+        cluster_sync();
+        // the cluster's sums of a place, in the order of the contraction indices; the CTAs share the tile's places out
+        const Tile t = tile_at(p, unit, 0, 1);
+        const Group& g = p.g[0];
+        const int rows = min(128, g.rows - 128 * t.m), items = rows * (BN / 4), steps0 = g.seg[0].steps;
+        const int end = (int)((long long)items * (share + 1) / shares);
+        for (int i = (int)((long long)items * share / shares) + tid; i < end; i += THREADS) {
+            const int r = i / (BN / 4), c = i % (BN / 4) * 4;
+            float4 a[8], b[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                a[q] = b[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (q < shares) {
+                    const int lo = (int)((long long)g.steps * q / shares), hi = (int)((long long)g.steps * (q + 1) / shares);
+                    if (lo < steps0) a[q] = kc::ld_cluster(sbase + r * SUMS_PITCH + c * 4, q);
+                    if (hi > steps0) b[q] = kc::ld_cluster(sbase + r * SUMS_PITCH + (BN + c) * 4, q);
+                }
+            }
+#pragma unroll
+            for (int q = 1; q < 8; ++q) {
+                a[0].x += a[q].x; a[0].y += a[q].y; a[0].z += a[q].z; a[0].w += a[q].w;
+                b[0].x += b[q].x; b[0].y += b[q].y; b[0].z += b[q].z; b[0].w += b[q].w;
+            }
+            float o[4] = {a[0].x, a[0].y, a[0].z, a[0].w};
+            by_act(p.act, [&](auto k) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] = act_value<decltype(k)::value>(o[j]);
+            });
+            if (p.gated) { o[0] *= b[0].x; o[1] *= b[0].y; o[2] *= b[0].z; o[3] *= b[0].w; }
+            const int col = t.n * BN + c;
+            if (col < g.cols)                         // (a multiple of 8)
+                *reinterpret_cast<uint2*>(p.y + (size_t)(128 * t.m + r) * g.cols + col) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
+        }
+        __syncwarp();
+        cluster_sync();                               // no CTA leaves while another reads its sums
+    }
     if (warp == 1) {
         tc_fence_after();
         if constexpr (CG == 2) tmem_dealloc_pair(tmem, 512);
@@ -801,36 +878,37 @@ inline void add_group(GemmParams& p, const Group& g)
     ++p.n_groups;
 }
 
-template <int CG, Epilogue EPI, bool WIDE>
-inline cudaError_t launch_one(const GemmParams& p, int n_sm, int dev, cudaStream_t st)
+template <int CG, Epilogue EPI, Mode MODE>
+inline cudaError_t launch_one(const GemmParams& p, int n_sm, int dev, cudaStream_t st, int cluster = CG)
 {
     static PerDeviceFlag attr_set;
     if (!attr_set.is_set(dev)) {
-        const cudaError_t e = cudaFuncSetAttribute(pair_gemm_kernel<CG, EPI, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+        const cudaError_t e = cudaFuncSetAttribute(pair_gemm_kernel<CG, EPI, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
         if (e != cudaSuccess) return e;
         attr_set.set(dev);
     }
-    const int units = n_sm / CG;
-    const unsigned grid = (unsigned)(CG * (p.n_tiles < units ? p.n_tiles : units));
-    return launch_pdl_cluster(pair_gemm_kernel<CG, EPI, WIDE>, grid, THREADS, SMEM, CG, st, p);
+    const int units = MODE == SPLIT_TILES ? p.n_tiles : n_sm / CG;
+    const unsigned grid = (unsigned)(cluster * (p.n_tiles < units ? p.n_tiles : units));
+    return launch_pdl_cluster(pair_gemm_kernel<CG, EPI, MODE>, grid, THREADS, SMEM, cluster, st, p);
 }
 template <Epilogue EPI>
-inline gf_status_t launch(int cg, const GemmParams& p, cudaStream_t st, std::atomic<uint64_t>* launches, bool wide = false)
+inline gf_status_t launch(int cg, const GemmParams& p, cudaStream_t st, std::atomic<uint64_t>* launches, Mode mode = TILES)
 {
     const int n_sm = sm_count(), dev = current_device();
     if (n_sm < 2 || dev < 0) return GF_ERR_CUDA;
     cudaError_t e = cudaErrorInvalidValue;
-    if (!wide) e = cg == 2 ? launch_one<2, EPI, false>(p, n_sm, dev, st) : launch_one<1, EPI, false>(p, n_sm, dev, st);
+    if (mode == TILES) e = cg == 2 ? launch_one<2, EPI, TILES>(p, n_sm, dev, st) : launch_one<1, EPI, TILES>(p, n_sm, dev, st);
     if constexpr (EPI == EPI_GATE || EPI == EPI_GATE_GRAD)
-        if (wide) e = launch_one<2, EPI, true>(p, n_sm, dev, st);
+        if (mode == WIDE_TILES) e = launch_one<2, EPI, WIDE_TILES>(p, n_sm, dev, st);
     launches->fetch_add(1, std::memory_order_relaxed);
     return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
 }
 
 // ---------------------------------------------------------------- several products in one launch (a gradient's)
-// Pairs of CTAs on 256 x 256 accumulators take 8 units of time per 64 contraction indices, single ones on 128 x 128 5: with a quarter of the
-// work and half the SMs they move twice the operand bytes per product.
-constexpr int STEP_TIME[3] = {0, 5, 8};
+// Time of 64 contraction indices, in units of 1/30 us.  An SM takes in 64 bytes per cycle: the 32 KB of its share of a pair's 256 x 256 products
+// take as long as these do, and the 32 KB of a 128 x 128 tile of its own hardly less (8192 deep, one tile: 0.264 us a step), for a
+// half of the work per SM.
+constexpr int STEP_TIME[3] = {0, 7, 8};
 
 struct Product {
     long long m, n;
