@@ -55,9 +55,8 @@ inline bool products(GemmParams& p, const Launch& l, const Shape& s, const __nv_
 //  - Products of half a tile's columns take 0.64 of a whole tile's step (16384 rows, 2048 and 7168 deep -> 2048: 520 us, wide 408; 8192
 //    rows, twice 512 -> 8192: 149, wide 126), a wide tile about two steps more for what its epilogue leaves (8192 rows, twice 256
 //    -> 8192: 103 and 101); where wide tiles are too few, half ones win (2048 rows, 768 and 2688 -> 768: 20 us, wide 25).
-//  - A tile that a cluster divides costs the joining, 2 us.  Clusters must lie within one GPC, so not every SM finds a place in one:
-//    four fifths of them do (see key_compress.cuh).
-inline Launch forward_launch(const Shape& s, int n_sm, bool may_split)
+//  - A tile that a cluster divides costs the joining, 2 us; all clusters have to run at one time (dev < 0: none are offered).
+inline Launch forward_launch(const Shape& s, int n_sm, int dev)
 {
     const long long m2 = ceil_div(s.rows, 256), m1 = ceil_div(s.rows, 128), s1 = ceil_div(s.K1, 64), s2 = ceil_div(s.K2, 64), both = s1 + s2;
     auto rounds = [&](long long tiles, int units) { return ceil_div(tiles, units); };
@@ -80,12 +79,8 @@ inline Launch forward_launch(const Shape& s, int n_sm, bool may_split)
         offer(1, TILES, 1, rounds(m1 * ceil_div(s.F, 64), n_sm) * both * 6);
     }
     const long long tiles = m1 * ceil_div(s.F, 128);
-    if (may_split && tiles * 2 * 5 <= n_sm * 4LL) {
-        long long c = n_sm * 4 / (5 * tiles);
-        if (c > 8) c = 8;
-        if (c > both / 2) c = both / 2;               // two steps for each CTA
-        if (c >= 2) offer(1, SPLIT_TILES, (int)c, ceil_div(both, c) * STEP_TIME[1] + 60);
-    }
+    for (int c = 8; dev >= 0 && c >= 2; --c)          // (two steps at least for each CTA)
+        if (tiles * c <= n_sm && both >= 2 * c && tiles <= clusters_at_once<EPI_GATE>(c, dev)) offer(1, SPLIT_TILES, c, ceil_div(both, c) * STEP_TIME[1] + 60);
     return best;
 }
 
@@ -101,7 +96,7 @@ inline gf_status_t gated_linear(const __nv_bfloat16* x, const __nv_bfloat16* w, 
     const int dev = current_device();
     if (dev < 0) return GF_ERR_CUDA;
     p.y = y;
-    gl::Launch l = gl::forward_launch(s, n_sm, true);
+    gl::Launch l = gl::forward_launch(s, n_sm, dev);
     if (!gl::products(p, l, s, x, w, x2, w2) || !pg::out_map(&p.out[0], y, s.rows, s.F)) return GF_ERR_CUDA;
     if (l.mode == pg::SPLIT_TILES) {
         if (pg::launch_one<1, pg::EPI_GATE, pg::SPLIT_TILES>(p, n_sm, dev, st, l.cluster) == cudaSuccess) {
@@ -109,7 +104,7 @@ inline gf_status_t gated_linear(const __nv_bfloat16* x, const __nv_bfloat16* w, 
             return GF_OK;
         }
         cudaGetLastError();                           // (no cluster can be placed, on a partitioned device: whole tiles)
-        l = gl::forward_launch(s, n_sm, false);
+        l = gl::forward_launch(s, n_sm, -1);
         p.n_groups = p.n_tiles = 0;
         if (!gl::products(p, l, s, x, w, x2, w2)) return GF_ERR_CUDA;
     }
@@ -154,7 +149,7 @@ inline gf_status_t gated_linear_backward(const __nv_bfloat16* x, const __nv_bflo
         GemmParams p = {};
         p.act = act;
         p.dy = dy;
-        const Launch l = forward_launch(s, n_sm, false);
+        const Launch l = forward_launch(s, n_sm, -1);
         if (!products(p, l, s, x, w, x2, w2) || !out_map(&p.out[0], da, s.rows, s.F) || (gated && !out_map(&p.out[1], db, s.rows, s.F))) return GF_ERR_CUDA;
         const gf_status_t e = launch<EPI_GATE_GRAD>(l.cg, p, st, launches, l.mode);
         if (e != GF_OK) return e;

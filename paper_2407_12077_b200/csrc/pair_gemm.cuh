@@ -239,8 +239,8 @@ __device__ __forceinline__ Tile tile_at(const GemmParams& p, int tile, int share
     t.slice = i / places;
     i -= t.slice * places;
     const int of = g.slices * shares, nth = t.slice + share;
-    t.lo = (int)((long long)g.steps * nth / of);
-    t.hi = (int)((long long)g.steps * (nth + 1) / of);
+    t.lo = g.steps * nth / of;                        // (steps < 2^25, of <= 32)
+    t.hi = g.steps * (nth + 1) / of;
     // bands of eight tiles along m, column by column: the tiles that run at one time share few rows of A and of B
     const int per = 8 * g.tiles_n, band = i / per, rest = i - band * per;
     const int h = min(8, g.tiles_m - 8 * band);
@@ -338,6 +338,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
     if constexpr (CG == 2) cluster_sync();            // the other CTA's barriers are there before anything arrives at them
     tc_fence_after();
     const uint32_t tmem = lds32(sbase + OFF_MISC + 8);
+    const Tile first = tile_at(p, unit, share, shares);       // (a unit has a tile at least)
 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (warp == 0) {
@@ -345,7 +346,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
         int s = 0, ph = 0, issued = 0;
         bool alive = true;
         for (int tile = unit; tile < p.n_tiles && alive; tile += units) {
-            const Tile t = tile_at(p, tile, share, shares);
+            const Tile t = tile == unit ? first : tile_at(p, tile, share, shares);
             const Group& g = p.g[t.g];
             const int m0 = t.m * 128 * CG + 128 * (int)rank, tn = t.n;
             for (int q = 0, at = 0; q < g.n_seg && alive; at += g.seg[q++].steps) {
@@ -400,7 +401,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
             int s = 0, ph = 0, ti = 0;
             bool alive = true;
             for (int tile = unit; tile < p.n_tiles && alive; tile += units, ++ti) {
-                const Tile t = tile_at(p, tile, share, shares);
+                const Tile t = tile == unit ? first : tile_at(p, tile, share, shares);
                 const Group& g = p.g[t.g];
                 const int set = SETS == 2 ? ti & 1 : 0, use = SETS == 2 ? ti >> 1 : ti;
                 // the epilogue has read this set's previous tile out of tensor memory
@@ -457,7 +458,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
         const uint32_t sl = sbase + OFF_SLAB + (warp - 2) * 4096;
         int ti = 0;
         for (int tile = unit; tile < p.n_tiles; tile += units, ++ti) {
-            const Tile place = tile_at(p, tile, share, shares);
+            const Tile place = tile == unit ? first : tile_at(p, tile, share, shares);
             const Group& g = p.g[place.g];
             const int tm = place.m, tn = place.n;
             const int row0 = tm * 128 * CG + 128 * (int)rank + 32 * sp, row = row0 + lane;
@@ -639,7 +640,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                     const int col = tn * width + c;
                     if (col >= g.cols) break;
                     take_slab();
-#pragma unroll
+#pragma unroll 1                                      // (a small call runs this code once: what it fetches of it counts)
                     for (int half = 0; half < 2; ++half) {
                         float a[32];
                         ld_acc(acc + c + 32 * half, a);
@@ -776,7 +777,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
             if constexpr (CG == 2) arrive_cluster_if(map_to_leader(bar(BAR_ACC_EMPTY + set)), lane == 0);
             else mbar_arrive_if(bar(BAR_ACC_EMPTY + set), lane == 0);
         }
-        if (lane == 0) bulk_wait<0>();
+        if (lane == 0) bulk_wait_read<0>();           // (shared memory may go; the grid's end completes the stores)
         __syncwarp();
     }
 
@@ -786,21 +787,22 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
     if constexpr (SPLIT) {
         cluster_sync();
         // the cluster's sums of a place, in the order of the contraction indices; the CTAs share the tile's places out
-        const Tile t = tile_at(p, unit, 0, 1);
         const Group& g = p.g[0];
-        const int rows = min(128, g.rows - 128 * t.m), items = rows * (BN / 4), steps0 = g.seg[0].steps;
-        const int end = (int)((long long)items * (share + 1) / shares);
-        for (int i = (int)((long long)items * share / shares) + tid; i < end; i += THREADS) {
+        const int rows = min(128, g.rows - 128 * first.m), items = rows * (BN / 4), steps0 = g.seg[0].steps;
+        int left_end = 0, right_begin = 0;            // shares 0 .. left_end-1 have products of the left, right_begin .. of the right
+        for (int q = 0; q < (int)shares; ++q) {
+            if (g.steps * q / (int)shares < steps0) left_end = q + 1;
+            if (g.steps * (q + 1) / (int)shares <= steps0) right_begin = q + 1;
+        }
+        const int end = items * (int)(share + 1) / (int)shares;
+        for (int i = items * (int)share / (int)shares + tid; i < end; i += THREADS) {
             const int r = i / (BN / 4), c = i % (BN / 4) * 4;
             float4 a[8], b[8];
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 a[q] = b[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (q < shares) {
-                    const int lo = (int)((long long)g.steps * q / shares), hi = (int)((long long)g.steps * (q + 1) / shares);
-                    if (lo < steps0) a[q] = kc::ld_cluster(sbase + r * SUMS_PITCH + c * 4, q);
-                    if (hi > steps0) b[q] = kc::ld_cluster(sbase + r * SUMS_PITCH + (BN + c) * 4, q);
-                }
+                if (q < left_end) a[q] = kc::ld_cluster(sbase + r * SUMS_PITCH + c * 4, q);
+                if (q >= right_begin && q < (int)shares) b[q] = kc::ld_cluster(sbase + r * SUMS_PITCH + (BN + c) * 4, q);
             }
 #pragma unroll
             for (int q = 1; q < 8; ++q) {
@@ -813,9 +815,9 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                 for (int j = 0; j < 4; ++j) o[j] = act_value<decltype(k)::value>(o[j]);
             });
             if (p.gated) { o[0] *= b[0].x; o[1] *= b[0].y; o[2] *= b[0].z; o[3] *= b[0].w; }
-            const int col = t.n * BN + c;
+            const int col = first.n * BN + c;
             if (col < g.cols)                         // (a multiple of 8)
-                *reinterpret_cast<uint2*>(p.y + (size_t)(128 * t.m + r) * g.cols + col) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
+                *reinterpret_cast<uint2*>(p.y + (size_t)(128 * first.m + r) * g.cols + col) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
         }
         __syncwarp();
         cluster_sync();                               // no CTA leaves while another reads its sums
@@ -891,6 +893,34 @@ inline cudaError_t launch_one(const GemmParams& p, int n_sm, int dev, cudaStream
     const unsigned grid = (unsigned)(cluster * (p.n_tiles < units ? p.n_tiles : units));
     return launch_pdl_cluster(pair_gemm_kernel<CG, EPI, MODE>, grid, THREADS, SMEM, cluster, st, p);
 }
+// Clusters of c CTAs (2 .. 8) that run at one time on the current device: they must lie within one GPC each, so it is fewer than the SMs
+// would hold.  0 where the device cannot tell.
+template <Epilogue EPI>
+inline int clusters_at_once(int c, int dev)
+{
+    static std::atomic<int> cached[MAX_DEVICES][9];           // value + 1; 0: not asked yet
+    const int known = cached[dev][c].load(std::memory_order_relaxed);
+    if (known) return known - 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(8 * c);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = SMEM;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)c;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaFuncSetAttribute(pair_gemm_kernel<1, EPI, SPLIT_TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, pair_gemm_kernel<1, EPI, SPLIT_TILES>, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        n = 0;
+    }
+    cached[dev][c].store(n + 1, std::memory_order_relaxed);
+    return n;
+}
+
 template <Epilogue EPI>
 inline gf_status_t launch(int cg, const GemmParams& p, cudaStream_t st, std::atomic<uint64_t>* launches, Mode mode = TILES)
 {
