@@ -3,316 +3,385 @@
 //     dy = rstd (g - mean(g) - xhat mean(g xhat)),   dgamma = sum over rows of dout * xhat,   dbeta = sum over rows of dout.
 // The statistics are taken from y again (it is read anyway), so the forward call keeps nothing.
 //
-// Bound by HBM (2 D elements in, D out per token).  As in the forward kernel a team of W warps owns whole rows and a lane the
-// 8-channel slices l + 32*W*j of them, raw slices of the next group being loaded while the current one is worked on; here a
-// lane also carries the sums of dgamma and dbeta over all its rows in registers (so at most four bf16 or two fp32 slices per lane:
-// y, dout, their prefetch and the sums fill the register file).  One exchange per row: each warp's mean, squared
-// deviations, sum of g and sum of g (y - its mean), joined by the pairwise formulae.  At the end a CTA adds its teams' sums up in
-// shared memory in a fixed order and leaves one row of each in the workspace; a second kernel adds those over the CTAs.
+// Bound by HBM (2 D elements in, D out per token).  A row's statistics want its elements side by side, the sums over rows want a column's
+// one below the other.  So rows come through a ring of three stages in shared memory (bulk copies of consecutive rows, up to 64 KB a
+// stage), and a stage is gone through twice:
+//  - along its rows: a warp (W warps for rows of more than 4 KB) takes one row's mean, squared deviations, sum of g and sum of
+//    g (y - mean) in registers, two true passes with a butterfly of shuffles after each; several warps' shares are joined by the
+//    pairwise formulae by the readers;
+//  - down its columns: a thread owns UPT units of 16 bytes of every row, writes their dy and carries the sums of dgamma and dbeta.
+// One barrier per stage between the two; behind it the stage before is refilled.  At the end a CTA leaves one row of sums in the
+// workspace; a second kernel adds those over the CTAs.
+// (A team of warps that keeps whole rows and all column sums in registers, with a barrier for each row, ran 16384 x 2048 bf16 in
+// 42.6 us with prefetches in registers and in 50.8 through a ring.)
+// Waits for copies are bounded (ck::mbar_wait): where one runs out, the status is raised and the CTA goes through its rows without
+// further waits, so that the warps that meet at barriers all come to them.
 #pragma once
 #include "ln_heads.cuh"
+#include "wkv6_chunked.cuh"
 
 namespace gf {
 namespace lng {
 
-using ln::Raw;
 using ln::add2;
 using ln::fma2;
 using ln::mul2;
-using ln::warp_sum;
 
-// bf16: eight warps with up to 255 registers a thread; fp32: sixteen with up to 128
-template <typename IO> constexpr int cta_threads() { return sizeof(IO) == 2 ? 256 : 512; }
-template <typename IO> constexpr int max_slices() { return sizeof(IO) == 2 ? 4 : 2; }
-constexpr int rows_per_group(int max_vpl, int vpl) { return max_vpl / vpl; }
+constexpr int STAGES = 3;
+constexpr int RING_STAGE_BYTES = 64 * 1024;             // of both tensors, at most, of all CTAs of an SM
+constexpr int MAX_CTAS = 2;                             // per SM
+constexpr int MAX_STAGE_ROWS = 64;
+template <typename IO> constexpr int per_unit() { return 16 / (int)sizeof(IO); }
 
-template <typename IO, int VPL, int W>
-constexpr int smem_bytes() { return VPL * 2 * 32 * W * 16 * 3; }      // gamma, and the sums of dgamma and dbeta, as float4 [VPL][2][32 W]
-
-template <typename IO, int VPL, int W>
-__global__ void __launch_bounds__(cta_threads<IO>(), 1)
-layernorm_heads_grad_kernel(const IO* __restrict__ y, const IO* __restrict__ dout, const float* __restrict__ gamma, float eps, IO* __restrict__ dy,
-                            float* __restrict__ sums, long long rows, int D)
+// eight bf16 or four fp32 values of shared memory
+template <typename IO> __device__ __forceinline__ void load_unit(uint32_t a, float2 (&f)[per_unit<IO>() / 2])
 {
-    constexpr int R = rows_per_group(max_slices<IO>(), VPL);
-    constexpr int THREADS = cta_threads<IO>();
-    constexpr int TEAMS = THREADS / 32 / W;
-    constexpr int TL = 32 * W;
-    extern __shared__ float4 sh[];                  // gamma [VPL][2][TL], dgamma, dbeta
-    __shared__ float4 part[TEAMS][2][R][W];         // per warp: mean, squared deviations, sum of g, sum of g (y - mean); by group parity
-    __shared__ float cnt[THREADS / 32];             // channels that each warp holds
+    uint32_t w[4];
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(a));
+    if constexpr (sizeof(IO) == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+    } else {
+        f[0] = make_float2(__uint_as_float(w[0]), __uint_as_float(w[1]));
+        f[1] = make_float2(__uint_as_float(w[2]), __uint_as_float(w[3]));
+    }
+}
+__device__ __forceinline__ void store_unit(__nv_bfloat16* p, const float2 (&f)[4]) { ln::store8(p, f); }
+__device__ __forceinline__ void store_unit(float* p, const float2 (&f)[2]) { __stcs(reinterpret_cast<float4*>(p), make_float4(f[0].x, f[0].y, f[1].x, f[1].y)); }
+
+// n bytes (a multiple of 16) of global memory into shared memory
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t n, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(n), "r"(bar) : "memory");
+}
+__device__ __forceinline__ float lanes_sum(float v, int lanes)      // over aligned groups of `lanes`
+{
+    for (int o = lanes / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// WARPS per CTA, CTAS per SM.  Along rows W warps share a row, a lane holds LU units of it; down columns a thread owns UPT units.
+// dynamic shared memory: gamma [D] as float4, then the ring [STAGES][y, dout][stage_rows][D], which the sums take over at the end
+template <typename IO, int WARPS, int CTAS, int LU, int W, int UPT>
+__global__ void __launch_bounds__(32 * WARPS, CTAS)
+layernorm_heads_grad_kernel(const IO* __restrict__ y, const IO* __restrict__ dout, const float* __restrict__ gamma, float eps, IO* __restrict__ dy,
+                            float* __restrict__ sums, long long rows, int D, int stage_rows, int row_lanes)
+{
+    constexpr int E = per_unit<IO>(), EH = E / 2, Q = E / 4;       // values, pairs and quads of a unit
+    constexpr int THREADS = 32 * WARPS;
+    static_assert(ln::MAX_D * 4 + STAGES * RING_STAGE_BYTES + 2 * MAX_STAGE_ROWS * 16 + (W > 1 ? WARPS * (WARPS / W) * 16 : 16) + 256 <= 232448, "shared memory budget of one sm_100 CTA");
+    extern __shared__ float4 sh[];
+    // by the stages' parity: per row its statistics (mean, rstd, mean g, mean g xhat), or per row and warp what they come from
+    // (mean, squared deviations, sum of g, sum of g (y - mean))
+    __shared__ float4 part[2][MAX_STAGE_ROWS];
+    __shared__ float4 joined[W > 1 ? WARPS : 1][W > 1 ? WARPS / W : 1];       // a row's statistics as each warp has joined them
+    __shared__ uint4 zero;                          // what a lane reads where the row has no unit for it
+    __shared__ float cnt[W];                        // channels of a row that each of its warps holds
+    __shared__ uint64_t full[STAGES];
+    __shared__ uint32_t misc[2];                    // abort word, wait limit
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int team = warp / W, wt = warp % W, tl = wt * 32 + lane;
-    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
-
-    for (int idx = tid; idx < VPL * 2 * TL; idx += THREADS) {
-        const int j = idx / (2 * TL), half = (idx / TL) & 1, l = idx % TL;
-        const int c = 8 * (l + TL * j) + 4 * half;
-        float4 gv = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c < D) gv = gamma ? *reinterpret_cast<const float4*>(gamma + c) : make_float4(1.f, 1.f, 1.f, 1.f);
-        sh[idx] = gv;
-        sh[VPL * 2 * TL + idx] = sh[2 * VPL * 2 * TL + idx] = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int units = D / E;
+    const uint32_t abort_flag = ck::smem_u32(misc), row_bytes = (uint32_t)D * sizeof(IO), tensor_bytes = stage_rows * row_bytes;
+    const uint32_t ring = ck::smem_u32(sh + D / 4), gammas = ck::smem_u32(sh);
+    auto bar = [&](int s) { return ck::smem_u32(&full[s]); };
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (tid == 0) {
+        for (int s = 0; s < STAGES; ++s) ck::mbar_init(bar(s), 1);
+        zero = make_uint4(0u, 0u, 0u, 0u);
+        ck::sts32(abort_flag, 0u);
+        ck::sts32(abort_flag + 4, ck::WAIT_LIMIT_US);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        ck::fence_proxy_async();
     }
-    int col[VPL];
-    bool on[VPL];
-    float mine = 0.f;
-#pragma unroll
-    for (int j = 0; j < VPL; ++j) {
-        col[j] = 8 * (tl + TL * j);
-        on[j] = col[j] < D;
-        mine += on[j] ? 8.f : 0.f;
-    }
-    const float n_w = warp_sum(mine), inv_nw = 1.f / n_w;   // every warp holds at least one slice (host picks W, VPL)
-    if (lane == 0) cnt[warp] = n_w;
-    __syncthreads();
-    const float inv_d = 1.f / (float)D;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    auto load_group = [&](Raw<IO> (&ry)[R][VPL], Raw<IO> (&rd)[R][VPL], long long r0) {
+    // the CTA's blocks of stage_rows rows: every gridDim.x-th
+    const long long n_blocks = (rows + stage_rows - 1) / stage_rows;
+    auto fetch = [&](long long b, int s) {          // by one thread
+        const long long r = b * stage_rows;
+        const uint32_t n = (uint32_t)min((long long)stage_rows, rows - r) * row_bytes, dst = ring + s * 2 * tensor_bytes;
+        ck::mbar_expect_tx(bar(s), 2 * n);
+        bulk_load(dst, y + (size_t)r * D, n, bar(s));
+        bulk_load(dst + tensor_bytes, dout + (size_t)r * D, n, bar(s));
+    };
+    if (tid == 0)
+        for (int s = 0; s < STAGES && blockIdx.x + (long long)s * gridDim.x < n_blocks; ++s) fetch(blockIdx.x + (long long)s * gridDim.x, s);
+    for (int i = tid; i < D / 4; i += THREADS) sh[i] = gamma ? reinterpret_cast<const float4*>(gamma)[i] : make_float4(1.f, 1.f, 1.f, 1.f);
+    auto gamma_of = [&](int unit, float2 (&g)[EH]) {
 #pragma unroll
-        for (int i = 0; i < R; ++i)
-#pragma unroll
-            for (int j = 0; j < VPL; ++j) {
-                if (on[j] && r0 + i < rows) {
-                    ln::load_raw(y + (size_t)(r0 + i) * D + col[j], ry[i][j]);
-                    ln::load_raw(dout + (size_t)(r0 + i) * D + col[j], rd[i][j]);
-                } else {
-                    ln::zero_raw(ry[i][j]);
-                    ln::zero_raw(rd[i][j]);
-                }
-            }
+        for (int q = 0; q < Q; ++q) {
+            const float4 v = ck::ldsf4(gammas + (unit * Q + q) * 16);
+            g[2 * q] = make_float2(v.x, v.y);
+            g[2 * q + 1] = make_float2(v.z, v.w);
+        }
     };
 
-    float2 dg[VPL][4], db[VPL][4];                  // this lane's sums over its rows
-#pragma unroll
-    for (int j = 0; j < VPL; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) dg[j][e] = db[j][e] = make_float2(0.f, 0.f);
-
-    const long long stride = (long long)gridDim.x * TEAMS * R;
-    long long r0 = ((long long)blockIdx.x * TEAMS + team) * R;
-    Raw<IO> ny[R][VPL], nd[R][VPL];
-    if (r0 < rows) load_group(ny, nd, r0);
-    int par = 0;
-    for (; r0 < rows; r0 += stride, par ^= 1) {
-        float2 x[R][VPL][4], d[R][VPL][4];
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-#pragma unroll
-            for (int j = 0; j < VPL; ++j) {
-                ln::unpack(ny[i][j], x[i][j]);
-                ln::unpack(nd[i][j], d[i][j]);
-            }
-        if (r0 + stride < rows) load_group(ny, nd, r0 + stride);
-
-        float mu[R], m2[R], sg[R], sgx[R];
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            float2 s2 = make_float2(0.f, 0.f), g2 = s2;
-#pragma unroll
-            for (int j = 0; j < VPL; ++j) {
-                const float4 g0 = sh[(2 * j) * TL + tl], g1 = sh[(2 * j + 1) * TL + tl];
-                const float2 gm[4] = {make_float2(g0.x, g0.y), make_float2(g0.z, g0.w), make_float2(g1.x, g1.y), make_float2(g1.z, g1.w)};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s2 = add2(s2, x[i][j][e]);
-                    g2 = fma2(d[i][j][e], gm[e], g2);
-                }
-            }
-            mu[i] = s2.x + s2.y;
-            sg[i] = g2.x + g2.y;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                mu[i] += __shfl_xor_sync(0xffffffffu, mu[i], o);
-                sg[i] += __shfl_xor_sync(0xffffffffu, sg[i], o);
-            }
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            mu[i] *= inv_nw;
-            const float2 neg_m = make_float2(-mu[i], -mu[i]);
-            float2 q2 = make_float2(0.f, 0.f), p2 = q2;
-#pragma unroll
-            for (int j = 0; j < VPL; ++j)
-                if (on[j]) {
-                    const float4 g0 = sh[(2 * j) * TL + tl], g1 = sh[(2 * j + 1) * TL + tl];
-                    const float2 gm[4] = {make_float2(g0.x, g0.y), make_float2(g0.z, g0.w), make_float2(g1.x, g1.y), make_float2(g1.z, g1.w)};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 c = add2(x[i][j][e], neg_m);
-                        q2 = fma2(c, c, q2);
-                        p2 = fma2(mul2(d[i][j][e], gm[e]), c, p2);
-                    }
-                }
-            m2[i] = q2.x + q2.y;
-            sgx[i] = p2.x + p2.y;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                m2[i] += __shfl_xor_sync(0xffffffffu, m2[i], o);
-                sgx[i] += __shfl_xor_sync(0xffffffffu, sgx[i], o);
-            }
-        if (W > 1) {
-            // ---- merge the team's warps: deviations from the common mean m are those from the warp's plus (its mean - m)
-            if (lane == 0) {
-#pragma unroll
-                for (int i = 0; i < R; ++i) part[team][par][i][wt] = make_float4(mu[i], m2[i], sg[i], sgx[i]);
-            }
-            asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(TL) : "memory");
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                float m = 0.f;
-#pragma unroll
-                for (int w = 0; w < W; ++w) m = fmaf(cnt[team * W + w], part[team][par][i][w].x, m);
-                m *= inv_d;
-                float q = 0.f, s = 0.f, p = 0.f;
-#pragma unroll
-                for (int w = 0; w < W; ++w) {
-                    const float4 pw = part[team][par][i][w];
-                    const float dm = pw.x - m;
-                    q += fmaf(cnt[team * W + w] * dm, dm, pw.y);
-                    s += pw.z;
-                    p += fmaf(pw.z, dm, pw.w);
-                }
-                mu[i] = m;
-                m2[i] = q;
-                sg[i] = s;
-                sgx[i] = p;
-            }
-            // part[team][par] is next written two groups on, after the barrier of the group between
-        }
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            if (r0 + i >= rows) break;
-            const float rstd = rsqrtf(fmaf(m2[i], inv_d, eps));
-            const float mg = sg[i] * inv_d, mgx = sgx[i] * rstd * inv_d;
-            const float2 neg_mu = make_float2(-mu[i], -mu[i]), r2 = make_float2(rstd, rstd);
-            const float2 neg_mg = make_float2(-mg, -mg), neg_mgx = make_float2(-mgx, -mgx);
-#pragma unroll
-            for (int j = 0; j < VPL; ++j)
-                if (on[j]) {
-                    const float4 g0 = sh[(2 * j) * TL + tl], g1 = sh[(2 * j + 1) * TL + tl];
-                    const float2 gm[4] = {make_float2(g0.x, g0.y), make_float2(g0.z, g0.w), make_float2(g1.x, g1.y), make_float2(g1.z, g1.w)};
-                    float2 o[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 xh = mul2(add2(x[i][j][e], neg_mu), r2);
-                        dg[j][e] = fma2(d[i][j][e], xh, dg[j][e]);
-                        db[j][e] = add2(db[j][e], d[i][j][e]);
-                        o[e] = mul2(fma2(xh, neg_mgx, fma2(d[i][j][e], gm[e], neg_mg)), r2);
-                    }
-                    ln::store8(dy + (size_t)(r0 + i) * D + col[j], o);
-                }
-        }
+    // along rows: this lane's units
+    const int piece = warp % W, per_warp = 32 / row_lanes;        // (W > 1: row_lanes is 32)
+    const int unit0 = W > 1 ? 32 * piece + lane : lane % row_lanes, unit_step = W > 1 ? 32 * W : row_lanes;
+    if (W > 1 && warp < W && lane == 0) {
+        int n = 0;
+        for (int u = 32 * warp; u < units; u += 32 * W) n += min(32, units - u);
+        cnt[warp] = (float)(n * E);
     }
+    __syncthreads();
+    uint32_t offset[LU];                            // of this lane's units in a row; past its end: none
+    bool has[LU];
+#pragma unroll
+    for (int j = 0; j < LU; ++j) {
+        const int u = unit0 + unit_step * j;
+        has[j] = u < units;
+        offset[j] = u * 16;
+    }
+    const uint32_t nothing = ck::smem_u32(&zero);
+    const float inv_d = 1.f / (float)D, inv_n = W > 1 ? 1.f / cnt[piece] : inv_d;
+
+    // down columns: this thread's units, and of every how many rows
+    const int groups = UPT > 1 ? 1 : THREADS / units, group = UPT > 1 ? 0 : tid / units;
+    int unit[UPT];
+    bool on[UPT];
+    float2 gm[UPT][EH], dg[UPT][EH], db[UPT][EH];
+#pragma unroll
+    for (int u = 0; u < UPT; ++u) {
+        unit[u] = UPT > 1 ? tid + THREADS * u : tid % units;
+        on[u] = UPT > 1 ? unit[u] < units : group < groups;
+        if (!on[u]) unit[u] = 0;
+        gamma_of(unit[u], gm[u]);
+#pragma unroll
+        for (int e = 0; e < EH; ++e) dg[u][e] = db[u][e] = make_float2(0.f, 0.f);
+    }
+
+    int s = 0, ph = 0, par = 0, prev = STAGES - 1;
+    bool alive = true;
+    for (long long b = blockIdx.x; b < n_blocks; b += gridDim.x, par ^= 1) {
+        alive = ck::mbar_wait_warp(bar(s), ph, abort_flag) && alive;
+        const int here = (int)min((long long)stage_rows, rows - b * stage_rows);
+        const uint32_t st = ring + s * 2 * tensor_bytes;
+        // ---- along rows
+        for (int r0 = W > 1 ? warp / W : warp * per_warp; r0 < here; r0 += W > 1 ? WARPS / W : WARPS * per_warp) {
+            const int r = W > 1 ? r0 : r0 + lane / row_lanes;
+            const bool in = r < here;
+            const uint32_t at = st + r * row_bytes;
+            float2 x[LU][EH];
+            float2 s2 = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int j = 0; j < LU; ++j) {
+                load_unit<IO>(in && has[j] ? at + offset[j] : nothing, x[j]);
+#pragma unroll
+                for (int e = 0; e < EH; ++e) s2 = add2(s2, x[j][e]);
+            }
+            const float mu = lanes_sum(s2.x + s2.y, row_lanes) * inv_n;
+            float2 q2 = make_float2(0.f, 0.f), g2 = q2, p2 = q2;
+#pragma unroll
+            for (int j = 0; j < LU; ++j) {
+                float2 d[EH], gj[EH];
+                load_unit<IO>(in && has[j] ? at + tensor_bytes + offset[j] : nothing, d);
+                gamma_of(has[j] ? unit0 + unit_step * j : 0, gj);
+                const float neg = has[j] ? -mu : 0.f;
+                const float2 neg_m = make_float2(neg, neg);
+#pragma unroll
+                for (int e = 0; e < EH; ++e) {
+                    const float2 c = add2(x[j][e], neg_m), g = mul2(d[e], gj[e]);
+                    q2 = fma2(c, c, q2);
+                    g2 = add2(g2, g);
+                    p2 = fma2(g, c, p2);
+                }
+            }
+            float m2 = q2.x + q2.y, sg = g2.x + g2.y, sgx = p2.x + p2.y;
+            for (int o = row_lanes / 2; o > 0; o >>= 1) {
+                m2 += __shfl_xor_sync(0xffffffffu, m2, o);
+                sg += __shfl_xor_sync(0xffffffffu, sg, o);
+                sgx += __shfl_xor_sync(0xffffffffu, sgx, o);
+            }
+            if (W > 1) {
+                if (lane == 0) part[par][r * W + piece] = make_float4(mu, m2, sg, sgx);
+            } else if (in && lane % row_lanes == 0) {
+                const float rstd = rsqrtf(fmaf(m2, inv_d, eps));
+                part[par][r] = make_float4(mu, rstd, sg * inv_d, sgx * rstd * inv_d);
+            }
+        }
+        __syncthreads();
+        // every warp has left the stage before
+        if (tid == 0 && alive && b != blockIdx.x && b + (long long)(STAGES - 1) * gridDim.x < n_blocks) fetch(b + (long long)(STAGES - 1) * gridDim.x, prev);
+        if (W > 1 && lane < here) {
+            // ---- a row's warps, joined: deviations from the common mean m are those from the warp's plus (its mean - m)
+            float m = 0.f, q = 0.f, sg = 0.f, p = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) m = fmaf(cnt[w], part[par][lane * W + w].x, m);
+            m *= inv_d;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float4 pw = part[par][lane * W + w];
+                const float dm = pw.x - m;
+                q += fmaf(cnt[w] * dm, dm, pw.y);
+                sg += pw.z;
+                p += fmaf(pw.z, dm, pw.w);
+            }
+            const float rstd = rsqrtf(fmaf(q, inv_d, eps));
+            joined[warp][lane] = make_float4(m, rstd, sg * inv_d, p * rstd * inv_d);
+        }
+        __syncwarp();
+        // ---- down columns
+        for (int r0 = 0; r0 < here; r0 += groups) {
+            const int r = min(r0 + group, here - 1);
+            const bool mine_too = r0 + group < here;
+            const float4 v = W > 1 ? joined[warp][r] : part[par][r];
+            const float2 neg_mu = make_float2(-v.x, -v.x), r2 = make_float2(v.y, v.y), neg_mg = make_float2(-v.z, -v.z), neg_mgx = make_float2(-v.w, -v.w);
+            IO* out = dy + (size_t)(b * stage_rows + r) * D;
+#pragma unroll
+            for (int u = 0; u < UPT; ++u)
+                if (on[u] && mine_too) {
+                    float2 x[EH], d[EH], o[EH];
+                    const uint32_t at = st + r * row_bytes + unit[u] * 16;
+                    load_unit<IO>(at, x);
+                    load_unit<IO>(at + tensor_bytes, d);
+#pragma unroll
+                    for (int e = 0; e < EH; ++e) {
+                        const float2 xh = mul2(add2(x[e], neg_mu), r2);
+                        dg[u][e] = fma2(d[e], xh, dg[u][e]);
+                        db[u][e] = add2(db[u][e], d[e]);
+                        o[e] = mul2(fma2(xh, neg_mgx, fma2(d[e], gm[u][e], neg_mg)), r2);
+                    }
+                    store_unit(out + unit[u] * E, o);
+                }
+        }
+        prev = s;
+        if (++s == STAGES) { s = 0; ph ^= 1; }
+    }
+    if (ck::lds32(abort_flag))                      // copies that are still under way land before the CTA leaves
+        for (int k = 0; k < STAGES; ++k)
+            if (blockIdx.x + (long long)k * gridDim.x < n_blocks) ck::mbar_wait_warp(bar(k), k < s ? ph ^ 1 : ph, abort_flag, false);
 
     if (!sums) return;
-    // ---- the CTA's sums: the teams one after another, each into its own lanes' places
-    float4* sg4 = sh + VPL * 2 * TL;
-    float4* sb4 = sg4 + VPL * 2 * TL;
-    for (int t = 0; t < TEAMS; ++t) {
-        __syncthreads();
-        if (team == t) {
-#pragma unroll
-            for (int j = 0; j < VPL; ++j)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int at = (2 * j + h) * TL + tl;
-                    float4 a = sg4[at], b = sb4[at];
-                    a.x += dg[j][2 * h].x; a.y += dg[j][2 * h].y; a.z += dg[j][2 * h + 1].x; a.w += dg[j][2 * h + 1].y;
-                    b.x += db[j][2 * h].x; b.y += db[j][2 * h].y; b.z += db[j][2 * h + 1].x; b.w += db[j][2 * h + 1].y;
-                    sg4[at] = a;
-                    sb4[at] = b;
-                }
-        }
-    }
-    __syncthreads();
     float* mine_g = sums + (size_t)blockIdx.x * 2 * D;
-    for (int idx = tid; idx < VPL * 2 * TL; idx += THREADS) {
-        const int j = idx / (2 * TL), half = (idx / TL) & 1, l = idx % TL;
-        const int c = 8 * (l + TL * j) + 4 * half;
-        if (c < D) {
-            *reinterpret_cast<float4*>(mine_g + c) = sg4[idx];
-            *reinterpret_cast<float4*>(mine_g + D + c) = sb4[idx];
+    if (groups == 1) {
+#pragma unroll
+        for (int u = 0; u < UPT; ++u)
+            if (on[u]) {
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    *reinterpret_cast<float4*>(mine_g + unit[u] * E + 4 * q) = make_float4(dg[u][2 * q].x, dg[u][2 * q].y, dg[u][2 * q + 1].x, dg[u][2 * q + 1].y);
+                    *reinterpret_cast<float4*>(mine_g + D + unit[u] * E + 4 * q) = make_float4(db[u][2 * q].x, db[u][2 * q].y, db[u][2 * q + 1].x, db[u][2 * q + 1].y);
+                }
+            }
+        return;
+    }
+    // ---- the groups' sums through shared memory: [value][thread], added up by the first group in order
+    __syncthreads();
+    float* hold = reinterpret_cast<float*>(sh + D / 4);
+#pragma unroll
+    for (int e = 0; e < EH; ++e) {
+        hold[(4 * e + 0) * THREADS + tid] = dg[0][e].x;
+        hold[(4 * e + 1) * THREADS + tid] = dg[0][e].y;
+        hold[(4 * e + 2) * THREADS + tid] = db[0][e].x;
+        hold[(4 * e + 3) * THREADS + tid] = db[0][e].y;
+    }
+    __syncthreads();
+    for (int i = tid; i < 2 * D; i += THREADS) {
+        const int c = i < D ? i : i - D, u = c / E, e = c % E;
+        const float* v = hold + (4 * (e / 2) + (i < D ? 0 : 2) + (e & 1)) * THREADS + u;
+        float t = 0.f;
+        for (int k = 0; k < groups; ++k) t += v[k * units];
+        mine_g[i] = t;
+    }
+}
+
+// sums [n][2 D] -> dgamma, dbeta (either may be nullptr).  A block takes 32 columns, eight lanes of four each; its 64 groups of lanes take every
+// 64th row, and the first adds the groups' sums up in order.
+constexpr int SUM_GROUPS = 64;
+__global__ void __launch_bounds__(8 * SUM_GROUPS) layernorm_heads_sum_kernel(const float* __restrict__ sums, int n, int D, float* __restrict__ dgamma, float* __restrict__ dbeta)
+{
+    __shared__ float4 part[SUM_GROUPS][8];
+    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+    const int group = threadIdx.x / 8, lane = threadIdx.x % 8, c = blockIdx.x * 32 + 4 * lane;
+    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c < 2 * D) {                                  // (D a multiple of 8: the four columns are all inside)
+#pragma unroll 5
+        for (int i = group; i < n; i += SUM_GROUPS) {
+            const float4 v = __ldcs(reinterpret_cast<const float4*>(sums + (size_t)i * 2 * D + c));
+            t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
         }
     }
-}
-
-// sums [n][2 D] -> dgamma, dbeta (either may be nullptr).  A block takes 32 columns, its warps every eighth row.
-__global__ void __launch_bounds__(256) layernorm_heads_sum_kernel(const float* __restrict__ sums, int n, int D, float* __restrict__ dgamma, float* __restrict__ dbeta)
-{
-    __shared__ float part[8][32];
-    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 32 + lane;
-    float s = 0.f;
-    if (c < 2 * D) {
-#pragma unroll 4
-        for (int i = warp; i < n; i += 8) s += sums[(size_t)i * 2 * D + c];
-    }
-    part[warp][lane] = s;
+    part[group][lane] = t;
     __syncthreads();
-    if (warp == 0 && c < 2 * D) {
+    if (threadIdx.x < 32 && blockIdx.x * 32 + threadIdx.x < 2 * D) {
+        const int k = blockIdx.x * 32 + threadIdx.x;
+        const float* v = reinterpret_cast<const float*>(part) + threadIdx.x;
+        float a[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 1; w < 8; ++w) s += part[w][lane];
-        if (c < D) {
-            if (dgamma) dgamma[c] = s;
-        } else if (dbeta) dbeta[c - D] = s;
+        for (int g = 0; g < SUM_GROUPS; ++g) a[g & 3] += v[g * 32];
+        const float sum = (a[0] + a[1]) + (a[2] + a[3]);
+        if (k < D) {
+            if (dgamma) dgamma[k] = sum;
+        } else if (dbeta) dbeta[k - D] = sum;
     }
 }
 
-template <typename IO, int VPL, int W>
+template <typename IO, int WARPS, int CTAS, int LU, int W, int UPT>
 inline cudaError_t launch(const IO* y, const IO* dout, const float* gamma, float eps, IO* dy, float* sums, long long rows, int D, int n_sm, unsigned* ctas, cudaStream_t st)
 {
-    constexpr int R = rows_per_group(max_slices<IO>(), VPL), TEAMS = cta_threads<IO>() / 32 / W, SMEM = smem_bytes<IO, VPL, W>();
-    if (SMEM + 4096 > 48 * 1024) {
-        static PerDeviceFlag attr_set;
-        const int dev = current_device();
-        if (dev < 0) return cudaErrorInvalidDevice;
-        if (!attr_set.is_set(dev)) {
-            const cudaError_t e = cudaFuncSetAttribute(layernorm_heads_grad_kernel<IO, VPL, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-            if (e != cudaSuccess) return e;
-            attr_set.set(dev);
-        }
+    const int row_bytes = D * (int)sizeof(IO), units = row_bytes / 16;
+    int row_lanes = 32;
+    while (row_lanes / 2 >= units) row_lanes /= 2;
+    // As many rows to a stage as it holds, but a pass of all warps along rows where few rows leave a CTA less than three stages; whole
+    // passes where it is several.
+    constexpr int STAGE_BYTES = RING_STAGE_BYTES / CTAS;
+    const int pass = W > 1 ? WARPS / W : WARPS * (32 / row_lanes);
+    int most = STAGE_BYTES / (2 * row_bytes);
+    if (most > MAX_STAGE_ROWS / W) most = MAX_STAGE_ROWS / W;
+    if (W > 1 && most > pass) most = pass;
+    if (most > pass) most = most / pass * pass;
+    const long long share = rows / (3LL * CTAS * n_sm);
+    int stage_rows = share >= most ? most : share < pass ? pass : (int)(share / pass * pass);
+    if (stage_rows > most) stage_rows = most;
+    n_sm *= CTAS;
+    const int ring = STAGES * 2 * stage_rows * row_bytes, hold = 4 * (per_unit<IO>() / 2) * 32 * WARPS * 4, smem = D * 4 + (ring > hold ? ring : hold);
+    static PerDeviceFlag attr_set;
+    const int dev = current_device();
+    if (dev < 0) return cudaErrorInvalidDevice;
+    if (!attr_set.is_set(dev)) {
+        const cudaError_t e = cudaFuncSetAttribute(layernorm_heads_grad_kernel<IO, WARPS, CTAS, LU, W, UPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (CTAS > 1 ? 16 * 1024 : ln::MAX_D * 4) + STAGES * STAGE_BYTES);
+        if (e != cudaSuccess) return e;
+        attr_set.set(dev);
     }
-    const long long groups = (rows + (long long)R * TEAMS - 1) / ((long long)R * TEAMS);
-    *ctas = (unsigned)(groups < n_sm ? groups : n_sm);
-    return launch_pdl(layernorm_heads_grad_kernel<IO, VPL, W>, *ctas, cta_threads<IO>(), SMEM, st, y, dout, gamma, eps, dy, sums, rows, D);
+    const long long blocks = (rows + stage_rows - 1) / stage_rows;
+    *ctas = (unsigned)(blocks < n_sm ? blocks : n_sm);
+    return launch_pdl(layernorm_heads_grad_kernel<IO, WARPS, CTAS, LU, W, UPT>, *ctas, 32 * WARPS, smem, st, y, dout, gamma, eps, dy, sums, rows, D, stage_rows, row_lanes);
 }
 
 }  // namespace lng
 
-// Workspace: one row of partial sums per CTA (at most one CTA per SM).
-inline size_t layernorm_heads_grad_bytes(int D, int n_sm) { return (size_t)n_sm * 2 * D * sizeof(float); }
+// Workspace: one row of partial sums per CTA.
+inline size_t layernorm_heads_grad_bytes(int D, int n_sm) { return (size_t)n_sm * lng::MAX_CTAS * 2 * D * sizeof(float); }
 
-// D a multiple of 8, at most ln::MAX_D.  The team is the narrowest that keeps to the slices a lane can hold.
+// D a multiple of 8, at most ln::MAX_D: up to 2048 units of 16 bytes.
 template <typename IO>
 inline gf_status_t layernorm_heads_grad(const IO* y, const IO* dout, const float* gamma, float eps, IO* dy, float* dgamma, float* dbeta, long long rows,
                                         int D, float* ws, int n_sm, cudaStream_t st, std::atomic<uint64_t>* launches)
 {
-    constexpr int MAX_VPL = lng::max_slices<IO>();
-    const int nvec = D / 8;
-    int w = 1;
-    while (32 * w * MAX_VPL < nvec) w *= 2;
-    const int vpl = (nvec + 32 * w - 1) / (32 * w);
+    const int units = D / lng::per_unit<IO>();
     float* sums = dgamma || dbeta ? ws : nullptr;
     cudaError_t e = cudaErrorInvalidValue;
     unsigned ctas = 0;
-#define GF_LNG_CASE(V, W_) \
-    if (vpl == V && w == W_) e = lng::launch<IO, V, W_>(y, dout, gamma, eps, dy, sums, rows, D, n_sm, &ctas, st);
-    if constexpr (MAX_VPL == 4) {
-        GF_LNG_CASE(1, 1) GF_LNG_CASE(2, 1) GF_LNG_CASE(3, 1) GF_LNG_CASE(4, 1)
-        GF_LNG_CASE(3, 2) GF_LNG_CASE(4, 2) GF_LNG_CASE(3, 4) GF_LNG_CASE(4, 4) GF_LNG_CASE(3, 8) GF_LNG_CASE(4, 8)
+    // Two CTAs per SM of eight warps with up to 128 registers: one's barrier and shuffles pass while the other computes (16384 x 2048
+    // bf16: one of sixteen warps 47.8 us).  Rows of more than 8 KB: one CTA, whose threads own more columns.
+#define GF_LNG_CASE(most, WARPS, CTAS, LU, W, UPT) \
+    else if (units <= most) e = lng::launch<IO, WARPS, CTAS, LU, W, UPT>(y, dout, gamma, eps, dy, sums, rows, D, n_sm, &ctas, st);
+    if (units <= 0) return GF_ERR_INVALID_ARG;
+    GF_LNG_CASE(32, 8, 2, 1, 1, 1) GF_LNG_CASE(64, 8, 2, 2, 1, 1) GF_LNG_CASE(96, 8, 2, 3, 1, 1) GF_LNG_CASE(128, 8, 2, 4, 1, 1)
+    GF_LNG_CASE(256, 8, 2, 4, 2, 1) GF_LNG_CASE(512, 8, 2, 4, 4, 2)
+    if constexpr (sizeof(IO) == 2) {
+        if (units <= 512) {}
+        GF_LNG_CASE(1024, 16, 1, 4, 8, 2)
     } else {
-        GF_LNG_CASE(1, 1) GF_LNG_CASE(2, 1) GF_LNG_CASE(2, 2) GF_LNG_CASE(2, 4) GF_LNG_CASE(2, 8) GF_LNG_CASE(2, 16)
+        if (units <= 512) {}
+        GF_LNG_CASE(1024, 8, 1, 8, 4, 4) GF_LNG_CASE(2048, 8, 1, 8, 8, 8)
     }
 #undef GF_LNG_CASE
     launches->fetch_add(1, std::memory_order_relaxed);
     if (e != cudaSuccess) return GF_ERR_CUDA;
     if (!sums) return GF_OK;
-    e = launch_pdl(lng::layernorm_heads_sum_kernel, (unsigned)((2 * D + 31) / 32), 256, 0, st, (const float*)sums, (int)ctas, D, dgamma, dbeta);
+    e = launch_pdl(lng::layernorm_heads_sum_kernel, (unsigned)((2 * D + 31) / 32), 8 * lng::SUM_GROUPS, 0, st, (const float*)sums, (int)ctas, D, dgamma, dbeta);
     launches->fetch_add(1, std::memory_order_relaxed);
     return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
 }
