@@ -12,8 +12,10 @@
 //  - down its columns: a thread owns UPT units of 16 bytes of every row, writes their dy and carries the sums of dgamma and dbeta.
 // One barrier per stage between the two; behind it the stage before is refilled.  At the end a CTA leaves one row of sums in the
 // workspace; a second kernel adds those over the CTAs.
-// (A team of warps that keeps whole rows and all column sums in registers, with a barrier for each row, ran 16384 x 2048 bf16 in
-// 42.6 us with prefetches in registers and in 50.8 through a ring.)
+// Measured: 10007 x 4096 fp32 77 us, 98 % of the copy rate; 16384 x 2048 bf16 43 us (71 %), 65536 rows 146 (84 %): half the bytes for the same
+// arithmetic, so bf16 rows wait on latency, and the launch, the ring's first fill and the sums (4 us) weigh more.  (A team of warps
+// that keeps whole rows and all column sums in registers, with a barrier for each row: the fp32 case 121 us with prefetches in
+// registers and 91 through a ring.)
 // Waits for copies are bounded (ck::mbar_wait): where one runs out, the status is raised and the CTA goes through its rows without
 // further waits, so that the warps that meet at barriers all come to them.
 #pragma once
@@ -31,6 +33,7 @@ constexpr int STAGES = 3;
 constexpr int RING_STAGE_BYTES = 64 * 1024;             // of both tensors, at most, of all CTAs of an SM
 constexpr int MAX_CTAS = 2;                             // per SM
 constexpr int MAX_STAGE_ROWS = 64;
+constexpr int gamma_bytes(int D) { return 4 * (D < ln::MAX_D ? D : ln::MAX_D); }       // at most
 template <typename IO> constexpr int per_unit() { return 16 / (int)sizeof(IO); }
 
 // eight bf16 or four fp32 values of shared memory
@@ -54,22 +57,16 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(n), "r"(bar) : "memory");
 }
-__device__ __forceinline__ float lanes_sum(float v, int lanes)      // over aligned groups of `lanes`
-{
-    for (int o = lanes / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
-
-// WARPS per CTA, CTAS per SM.  Along rows W warps share a row, a lane holds LU units of it; down columns a thread owns UPT units.
+// WARPS per CTA, CTAS per SM.  Along rows W warps share a row, a lane holds LU units of it, RB rows at a time; down columns a thread owns UPT units.
 // dynamic shared memory: gamma [D] as float4, then the ring [STAGES][y, dout][stage_rows][D], which the sums take over at the end
-template <typename IO, int WARPS, int CTAS, int LU, int W, int UPT>
+template <typename IO, int WARPS, int CTAS, int LU, int W, int UPT, int RB>
 __global__ void __launch_bounds__(32 * WARPS, CTAS)
 layernorm_heads_grad_kernel(const IO* __restrict__ y, const IO* __restrict__ dout, const float* __restrict__ gamma, float eps, IO* __restrict__ dy,
                             float* __restrict__ sums, long long rows, int D, int stage_rows, int row_lanes)
 {
     constexpr int E = per_unit<IO>(), EH = E / 2, Q = E / 4;       // values, pairs and quads of a unit
     constexpr int THREADS = 32 * WARPS;
-    static_assert(ln::MAX_D * 4 + STAGES * RING_STAGE_BYTES + 2 * MAX_STAGE_ROWS * 16 + (W > 1 ? WARPS * (WARPS / W) * 16 : 16) + 256 <= 232448, "shared memory budget of one sm_100 CTA");
+    static_assert(gamma_bytes(E * THREADS * UPT) + STAGES * RING_STAGE_BYTES / CTAS + 2 * MAX_STAGE_ROWS * 16 + (W > 1 ? WARPS * (WARPS / W) * 16 : 16) + 256 <= 232448 / CTAS, "shared memory of an SM");
     extern __shared__ float4 sh[];
     // by the stages' parity: per row its statistics (mean, rstd, mean g, mean g xhat), or per row and warp what they come from
     // (mean, squared deviations, sum of g, sum of g (y - mean))
@@ -117,7 +114,7 @@ layernorm_heads_grad_kernel(const IO* __restrict__ y, const IO* __restrict__ dou
     };
 
     // along rows: this lane's units
-    const int piece = warp % W, per_warp = 32 / row_lanes;        // (W > 1: row_lanes is 32)
+    const int piece = warp % W, per_warp = 32 / row_lanes, row_step = W > 1 ? WARPS / W : WARPS * per_warp;        // (W > 1: row_lanes is 32)
     const int unit0 = W > 1 ? 32 * piece + lane : lane % row_lanes, unit_step = W > 1 ? 32 * W : row_lanes;
     if (W > 1 && warp < W && lane == 0) {
         int n = 0;
@@ -158,46 +155,76 @@ layernorm_heads_grad_kernel(const IO* __restrict__ y, const IO* __restrict__ dou
         const int here = (int)min((long long)stage_rows, rows - b * stage_rows);
         const uint32_t st = ring + s * 2 * tensor_bytes;
         // ---- along rows
-        for (int r0 = W > 1 ? warp / W : warp * per_warp; r0 < here; r0 += W > 1 ? WARPS / W : WARPS * per_warp) {
-            const int r = W > 1 ? r0 : r0 + lane / row_lanes;
-            const bool in = r < here;
-            const uint32_t at = st + r * row_bytes;
-            float2 x[LU][EH];
-            float2 s2 = make_float2(0.f, 0.f);
+        // (RB rows at a time where they are short: their loads and shuffles hide one another's latency)
+        for (int r0 = W > 1 ? warp / W : warp * per_warp; r0 < here; r0 += RB * row_step) {
+            float2 x[RB][LU][EH];
+            float mu[RB], m2[RB], sg[RB], sgx[RB];
+            bool in[RB];
+            uint32_t at[RB];
 #pragma unroll
-            for (int j = 0; j < LU; ++j) {
-                load_unit<IO>(in && has[j] ? at + offset[j] : nothing, x[j]);
+            for (int i = 0; i < RB; ++i) {
+                const int r = r0 + i * row_step + (W > 1 ? 0 : lane / row_lanes);
+                in[i] = r < here;
+                at[i] = st + r * row_bytes;
+                float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int e = 0; e < EH; ++e) s2 = add2(s2, x[j][e]);
+                for (int j = 0; j < LU; ++j) {
+                    load_unit<IO>(in[i] && has[j] ? at[i] + offset[j] : nothing, x[i][j]);
+#pragma unroll
+                    for (int e = 0; e < EH; ++e) s2 = add2(s2, x[i][j][e]);
+                }
+                mu[i] = s2.x + s2.y;
             }
-            const float mu = lanes_sum(s2.x + s2.y, row_lanes) * inv_n;
-            float2 q2 = make_float2(0.f, 0.f), g2 = q2, p2 = q2;
+            for (int o = row_lanes / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int i = 0; i < RB; ++i) mu[i] += __shfl_xor_sync(0xffffffffu, mu[i], o);
+            float2 q2[RB], g2[RB], p2[RB];
+#pragma unroll
+            for (int i = 0; i < RB; ++i) {
+                mu[i] *= inv_n;
+                q2[i] = g2[i] = p2[i] = make_float2(0.f, 0.f);
+            }
 #pragma unroll
             for (int j = 0; j < LU; ++j) {
-                float2 d[EH], gj[EH];
-                load_unit<IO>(in && has[j] ? at + tensor_bytes + offset[j] : nothing, d);
+                float2 gj[EH];
                 gamma_of(has[j] ? unit0 + unit_step * j : 0, gj);
-                const float neg = has[j] ? -mu : 0.f;
-                const float2 neg_m = make_float2(neg, neg);
 #pragma unroll
-                for (int e = 0; e < EH; ++e) {
-                    const float2 c = add2(x[j][e], neg_m), g = mul2(d[e], gj[e]);
-                    q2 = fma2(c, c, q2);
-                    g2 = add2(g2, g);
-                    p2 = fma2(g, c, p2);
+                for (int i = 0; i < RB; ++i) {
+                    float2 d[EH];
+                    load_unit<IO>(in[i] && has[j] ? at[i] + tensor_bytes + offset[j] : nothing, d);
+                    const float neg = has[j] ? -mu[i] : 0.f;
+                    const float2 neg_m = make_float2(neg, neg);
+#pragma unroll
+                    for (int e = 0; e < EH; ++e) {
+                        const float2 c = add2(x[i][j][e], neg_m), g = mul2(d[e], gj[e]);
+                        q2[i] = fma2(c, c, q2[i]);
+                        g2[i] = add2(g2[i], g);
+                        p2[i] = fma2(g, c, p2[i]);
+                    }
                 }
             }
-            float m2 = q2.x + q2.y, sg = g2.x + g2.y, sgx = p2.x + p2.y;
-            for (int o = row_lanes / 2; o > 0; o >>= 1) {
-                m2 += __shfl_xor_sync(0xffffffffu, m2, o);
-                sg += __shfl_xor_sync(0xffffffffu, sg, o);
-                sgx += __shfl_xor_sync(0xffffffffu, sgx, o);
+#pragma unroll
+            for (int i = 0; i < RB; ++i) {
+                m2[i] = q2[i].x + q2[i].y;
+                sg[i] = g2[i].x + g2[i].y;
+                sgx[i] = p2[i].x + p2[i].y;
             }
-            if (W > 1) {
-                if (lane == 0) part[par][r * W + piece] = make_float4(mu, m2, sg, sgx);
-            } else if (in && lane % row_lanes == 0) {
-                const float rstd = rsqrtf(fmaf(m2, inv_d, eps));
-                part[par][r] = make_float4(mu, rstd, sg * inv_d, sgx * rstd * inv_d);
+            for (int o = row_lanes / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int i = 0; i < RB; ++i) {
+                    m2[i] += __shfl_xor_sync(0xffffffffu, m2[i], o);
+                    sg[i] += __shfl_xor_sync(0xffffffffu, sg[i], o);
+                    sgx[i] += __shfl_xor_sync(0xffffffffu, sgx[i], o);
+                }
+#pragma unroll
+            for (int i = 0; i < RB; ++i) {
+                const int r = r0 + i * row_step + (W > 1 ? 0 : lane / row_lanes);
+                if (W > 1) {
+                    if (in[i] && lane == 0) part[par][r * W + piece] = make_float4(mu[i], m2[i], sg[i], sgx[i]);
+                } else if (in[i] && lane % row_lanes == 0) {
+                    const float rstd = rsqrtf(fmaf(m2[i], inv_d, eps));
+                    part[par][r] = make_float4(mu[i], rstd, sg[i] * inv_d, sgx[i] * rstd * inv_d);
+                }
             }
         }
         __syncthreads();
@@ -222,6 +249,7 @@ layernorm_heads_grad_kernel(const IO* __restrict__ y, const IO* __restrict__ dou
         }
         __syncwarp();
         // ---- down columns
+#pragma unroll 2
         for (int r0 = 0; r0 < here; r0 += groups) {
             const int r = min(r0 + group, here - 1);
             const bool mine_too = r0 + group < here;
@@ -317,7 +345,7 @@ __global__ void __launch_bounds__(8 * SUM_GROUPS) layernorm_heads_sum_kernel(con
     }
 }
 
-template <typename IO, int WARPS, int CTAS, int LU, int W, int UPT>
+template <typename IO, int WARPS, int CTAS, int LU, int W, int UPT, int RB>
 inline cudaError_t launch(const IO* y, const IO* dout, const float* gamma, float eps, IO* dy, float* sums, long long rows, int D, int n_sm, unsigned* ctas, cudaStream_t st)
 {
     const int row_bytes = D * (int)sizeof(IO), units = row_bytes / 16;
@@ -326,10 +354,10 @@ inline cudaError_t launch(const IO* y, const IO* dout, const float* gamma, float
     // As many rows to a stage as it holds, but a pass of all warps along rows where few rows leave a CTA less than three stages; whole
     // passes where it is several.
     constexpr int STAGE_BYTES = RING_STAGE_BYTES / CTAS;
-    const int pass = W > 1 ? WARPS / W : WARPS * (32 / row_lanes);
+    const int pass = RB * (W > 1 ? WARPS / W : WARPS * (32 / row_lanes));
     int most = STAGE_BYTES / (2 * row_bytes);
     if (most > MAX_STAGE_ROWS / W) most = MAX_STAGE_ROWS / W;
-    if (W > 1 && most > pass) most = pass;
+    if (W > 1 && most > WARPS / W) most = WARPS / W;
     if (most > pass) most = most / pass * pass;
     const long long share = rows / (3LL * CTAS * n_sm);
     int stage_rows = share >= most ? most : share < pass ? pass : (int)(share / pass * pass);
@@ -340,13 +368,13 @@ inline cudaError_t launch(const IO* y, const IO* dout, const float* gamma, float
     const int dev = current_device();
     if (dev < 0) return cudaErrorInvalidDevice;
     if (!attr_set.is_set(dev)) {
-        const cudaError_t e = cudaFuncSetAttribute(layernorm_heads_grad_kernel<IO, WARPS, CTAS, LU, W, UPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (CTAS > 1 ? 16 * 1024 : ln::MAX_D * 4) + STAGES * STAGE_BYTES);
+        const cudaError_t e = cudaFuncSetAttribute(layernorm_heads_grad_kernel<IO, WARPS, CTAS, LU, W, UPT, RB>, cudaFuncAttributeMaxDynamicSharedMemorySize, gamma_bytes(per_unit<IO>() * 32 * WARPS * UPT) + STAGES * STAGE_BYTES);
         if (e != cudaSuccess) return e;
         attr_set.set(dev);
     }
     const long long blocks = (rows + stage_rows - 1) / stage_rows;
     *ctas = (unsigned)(blocks < n_sm ? blocks : n_sm);
-    return launch_pdl(layernorm_heads_grad_kernel<IO, WARPS, CTAS, LU, W, UPT>, *ctas, 32 * WARPS, smem, st, y, dout, gamma, eps, dy, sums, rows, D, stage_rows, row_lanes);
+    return launch_pdl(layernorm_heads_grad_kernel<IO, WARPS, CTAS, LU, W, UPT, RB>, *ctas, 32 * WARPS, smem, st, y, dout, gamma, eps, dy, sums, rows, D, stage_rows, row_lanes);
 }
 
 }  // namespace lng
@@ -363,19 +391,19 @@ inline gf_status_t layernorm_heads_grad(const IO* y, const IO* dout, const float
     float* sums = dgamma || dbeta ? ws : nullptr;
     cudaError_t e = cudaErrorInvalidValue;
     unsigned ctas = 0;
-    // Two CTAs per SM of eight warps with up to 128 registers: one's barrier and shuffles pass while the other computes (16384 x 2048
-    // bf16: one of sixteen warps 47.8 us).  Rows of more than 8 KB: one CTA, whose threads own more columns.
-#define GF_LNG_CASE(most, WARPS, CTAS, LU, W, UPT) \
-    else if (units <= most) e = lng::launch<IO, WARPS, CTAS, LU, W, UPT>(y, dout, gamma, eps, dy, sums, rows, D, n_sm, &ctas, st);
+    // Two small CTAs per SM where their columns' sums fit: one's barrier and shuffles pass while the other computes (65536 x 2048 bf16: one of
+    // sixteen warps 150 us, two of eight 150, two of four 146; 65536 x 768: 72, 72, 75).  Rows of more than 4 KB: one CTA, whose threads
+    // own more columns (16384 x 4096 bf16 81 us, two of eight warps 112).  Short rows two at a time (200000 x 64: 26.6 us, one 34).
+#define GF_LNG_CASE(most, WARPS, CTAS, LU, W, UPT, RB) \
+    else if (units <= most) e = lng::launch<IO, WARPS, CTAS, LU, W, UPT, RB>(y, dout, gamma, eps, dy, sums, rows, D, n_sm, &ctas, st);
     if (units <= 0) return GF_ERR_INVALID_ARG;
-    GF_LNG_CASE(32, 8, 2, 1, 1, 1) GF_LNG_CASE(64, 8, 2, 2, 1, 1) GF_LNG_CASE(96, 8, 2, 3, 1, 1) GF_LNG_CASE(128, 8, 2, 4, 1, 1)
-    GF_LNG_CASE(256, 8, 2, 4, 2, 1) GF_LNG_CASE(512, 8, 2, 4, 4, 2)
+    GF_LNG_CASE(32, 8, 2, 1, 1, 1, 2) GF_LNG_CASE(64, 8, 2, 2, 1, 1, 2) GF_LNG_CASE(96, 16, 1, 3, 1, 1, 1) GF_LNG_CASE(128, 8, 2, 4, 1, 1, 1)
     if constexpr (sizeof(IO) == 2) {
-        if (units <= 512) {}
-        GF_LNG_CASE(1024, 16, 1, 4, 8, 2)
+        if (units <= 128) {}
+        GF_LNG_CASE(256, 4, 2, 8, 1, 2, 1) GF_LNG_CASE(512, 8, 1, 8, 2, 2, 1) GF_LNG_CASE(1024, 16, 1, 4, 8, 2, 1)
     } else {
-        if (units <= 512) {}
-        GF_LNG_CASE(1024, 8, 1, 8, 4, 4) GF_LNG_CASE(2048, 8, 1, 8, 8, 8)
+        if (units <= 128) {}
+        GF_LNG_CASE(256, 8, 2, 4, 2, 1, 1) GF_LNG_CASE(512, 16, 1, 4, 4, 1, 1) GF_LNG_CASE(1024, 8, 1, 8, 4, 4, 1) GF_LNG_CASE(2048, 8, 1, 8, 8, 8, 1)
     }
 #undef GF_LNG_CASE
     launches->fetch_add(1, std::memory_order_relaxed);
