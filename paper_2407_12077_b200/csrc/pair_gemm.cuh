@@ -164,13 +164,31 @@ __device__ __forceinline__ uint32_t instr_desc(int m, int n, bool a_mn, bool b_m
 }
 
 // ---------------------------------------------------------------- activations
+// The normal distribution Phi(a) by the Chebyshev fit of the complementary error function in Press et al., Numerical Recipes (erfcc): a relative error
+// of 1.2e-7 on the whole axis, and of 4e-6 (|a| < 8) with the exponential's argument in fp32, far below a bf16 rounding.  Fourteen
+// instructions where erfcf takes some forty (8192 rows, twice 512 deep -> 8192, with gelu: 220 us -> 164).
+__device__ __forceinline__ float normal_cdf(float a)
+{
+    const float x = fabsf(a) * 0.70710678f, t = __fdividef(1.f, fmaf(0.5f, x, 1.f));
+    float p = fmaf(0.17087277f, t, -0.82215223f);
+    p = fmaf(p, t, 1.48851587f);
+    p = fmaf(p, t, -1.13520398f);
+    p = fmaf(p, t, 0.27886807f);
+    p = fmaf(p, t, -0.18628806f);
+    p = fmaf(p, t, 0.09678418f);
+    p = fmaf(p, t, 0.37409196f);
+    p = fmaf(p, t, 1.00002368f);
+    p = fmaf(p, t, -1.26551223f);
+    const float q = 0.5f * t * ex2(fmaf(-x, x, p) * LOG2E);
+    return a < 0.f ? q : 1.f - q;
+}
 template <int ACT> __device__ __forceinline__ float act_value(float a)
 {
     if constexpr (ACT == ACT_RELU2) {
         const float r = a != a ? a : fmaxf(a, 0.f);
         return r * r;
     } else if constexpr (ACT == ACT_GELU) {
-        return a * (0.5f * erfcf(a * -0.70710678f));
+        return a * normal_cdf(a);
     } else {
         const float s = __fdividef(1.f, 1.f + __expf(-a));
         return ACT == ACT_SIGMOID ? s : a * s;
@@ -184,7 +202,7 @@ template <int ACT> __device__ __forceinline__ void act_grad(float a, float& f, f
         f = r * r;
         df = 2.f * r;
     } else if constexpr (ACT == ACT_GELU) {
-        const float phi = 0.5f * erfcf(a * -0.70710678f);
+        const float phi = normal_cdf(a);
         f = a * phi;
         df = fmaf(a * 0.39894228f, __expf(-0.5f * a * a), phi);
     } else {
