@@ -27,12 +27,6 @@ inline int choose_cg(long long large, long long small, int n_sm)
     return ceil_div(large, n_sm / 2) * STEP_TIME[2] <= ceil_div(small, n_sm) * STEP_TIME[1] ? 2 : 1;
 }
 
-struct Launch {
-    int cg;
-    Mode mode;
-    int cluster;                    // SPLIT_TILES
-};
-
 // Both products of every column (maps 0: x, 1: w, 2: w2, 3: x2; all as they lie in memory, weights [K][F]).
 inline bool products(GemmParams& p, const Launch& l, const Shape& s, const __nv_bfloat16* x, const __nv_bfloat16* w, const __nv_bfloat16* x2, const __nv_bfloat16* w2)
 {
@@ -48,6 +42,7 @@ inline bool products(GemmParams& p, const Launch& l, const Shape& s, const __nv_
         add_segment(g, segment(3, false, 2, true, s.K2, whole ? B_WHOLE : B_HALF, true));
     }
     p.gated = gated;
+    p.n_groups = p.n_tiles = 0;
     add_group(p, g);
     return true;
 }
@@ -55,11 +50,12 @@ inline bool products(GemmParams& p, const Launch& l, const Shape& s, const __nv_
 //  - Products of half a tile's columns take 0.64 of a whole tile's step (16384 rows, 2048 and 7168 deep -> 2048: 520 us, wide 408; 8192
 //    rows, twice 512 -> 8192: 149, wide 126), a wide tile about two steps more for what its epilogue leaves (8192 rows, twice 256
 //    -> 8192: 103 and 101); where wide tiles are too few, half ones win (2048 rows, 768 and 2688 -> 768: 20 us, wide 25).
-//  - A tile that a cluster divides costs the joining, 2 us; all clusters have to run at one time (dev < 0: none are offered).
-inline Launch forward_launch(const Shape& s, int n_sm, int dev)
+//  - A tile that a cluster divides costs the joining, 2 us; all clusters have to run at one time.
+inline Launch forward_launch(const Shape& s, int n_sm, bool clusters, bool split)
 {
     const long long m2 = ceil_div(s.rows, 256), m1 = ceil_div(s.rows, 128), s1 = ceil_div(s.K1, 64), s2 = ceil_div(s.K2, 64), both = s1 + s2;
     auto rounds = [&](long long tiles, int units) { return ceil_div(tiles, units); };
+    if (!clusters) return SINGLE;
     Launch best = {2, TILES, 2};
     long long time;
     auto offer = [&](int cg, Mode mode, int cluster, long long t) {
@@ -79,8 +75,8 @@ inline Launch forward_launch(const Shape& s, int n_sm, int dev)
         offer(1, TILES, 1, rounds(m1 * ceil_div(s.F, 64), n_sm) * both * 6);
     }
     const long long tiles = m1 * ceil_div(s.F, 128);
-    for (int c = 8; dev >= 0 && c >= 2; --c)          // (two steps at least for each CTA)
-        if (tiles * c <= n_sm && both >= 2 * c && tiles <= clusters_at_once<EPI_GATE>(c, dev)) offer(1, SPLIT_TILES, c, ceil_div(both, c) * STEP_TIME[1] + 60);
+    for (int c = 8; split && c >= 2; --c)          // (two steps at least for each CTA)
+        if (tiles * c <= n_sm && both >= 2 * c && tiles <= clusters_at_once(c, n_sm)) offer(1, SPLIT_TILES, c, ceil_div(both, c) * STEP_TIME[1] + 60);
     return best;
 }
 
@@ -93,22 +89,14 @@ inline gf_status_t gated_linear(const __nv_bfloat16* x, const __nv_bfloat16* w, 
     if (n_sm < 2) return GF_ERR_CUDA;
     pg::GemmParams p = {};
     p.act = act;
-    const int dev = current_device();
-    if (dev < 0) return GF_ERR_CUDA;
     p.y = y;
-    gl::Launch l = gl::forward_launch(s, n_sm, dev);
-    if (!gl::products(p, l, s, x, w, x2, w2) || !pg::out_map(&p.out[0], y, s.rows, s.F)) return GF_ERR_CUDA;
-    if (l.mode == pg::SPLIT_TILES) {
-        if (pg::launch_one<1, pg::EPI_GATE, pg::SPLIT_TILES>(p, n_sm, dev, st, l.cluster) == cudaSuccess) {
-            launches->fetch_add(1, std::memory_order_relaxed);
-            return GF_OK;
-        }
-        cudaGetLastError();                           // (no cluster can be placed, on a partitioned device: whole tiles)
-        l = gl::forward_launch(s, n_sm, -1);
-        p.n_groups = p.n_tiles = 0;
+    if (!pg::out_map(&p.out[0], y, s.rows, s.F)) return GF_ERR_CUDA;
+    for (const bool clusters : {true, false}) {       // (without any where the device refuses them)
+        const pg::Launch l = gl::forward_launch(s, n_sm, clusters, true);
         if (!gl::products(p, l, s, x, w, x2, w2)) return GF_ERR_CUDA;
+        if (pg::launch<pg::EPI_GATE>(l, p, st, launches)) return GF_OK;
     }
-    return pg::launch<pg::EPI_GATE>(l.cg, p, st, launches, l.mode);
+    return GF_ERR_CUDA;
 }
 
 namespace gl {
@@ -145,21 +133,23 @@ inline gf_status_t gated_linear_backward(const __nv_bfloat16* x, const __nv_bflo
     if (n_sm < 2) return GF_ERR_CUDA;
     const bool gated = s.K2 > 0;
     __nv_bfloat16 *da = ws, *db = ws + (size_t)s.rows * s.F;
-    {
+    bool done = false;
+    for (const bool clusters : {true, false}) {
         GemmParams p = {};
         p.act = act;
         p.dy = dy;
-        const Launch l = forward_launch(s, n_sm, -1);
+        const Launch l = forward_launch(s, n_sm, clusters, false);
         if (!products(p, l, s, x, w, x2, w2) || !out_map(&p.out[0], da, s.rows, s.F) || (gated && !out_map(&p.out[1], db, s.rows, s.F))) return GF_ERR_CUDA;
-        const gf_status_t e = launch<EPI_GATE_GRAD>(l.cg, p, st, launches, l.mode);
-        if (e != GF_OK) return e;
+        if ((done = launch<EPI_GATE_GRAD>(l, p, st, launches))) break;
     }
+    if (!done) return GF_ERR_CUDA;
     GemmParams p = {};
     if (!in_map(&p.in[0], da, s.rows, s.F) || !in_map(&p.in[2], w, s.K1, s.F) || !in_map(&p.in[4], x, s.rows, s.K1)) return GF_ERR_CUDA;
     if (gated && (!in_map(&p.in[1], db, s.rows, s.F) || !in_map(&p.in[3], w2, s.K2, s.F) || !in_map(&p.in[5], x2, s.rows, s.K2))) return GF_ERR_CUDA;
     Product q[MAX_GROUPS];
     const int n = gradient_products(s, q, dx, dw, dx2, dw2);
-    return run_products(p, q, n, plan_products(q, n, plan_sms(), false), PART_ONLY, reinterpret_cast<char*>(ws) + operand_bytes(s), st, launches);
+    Plan plan = plan_products(q, n, plan_sms(), false);
+    return run_products(p, q, n, plan, PART_ONLY, reinterpret_cast<char*>(ws) + operand_bytes(s), st, launches);
 }
 
 }  // namespace gf

@@ -911,45 +911,39 @@ inline cudaError_t launch_one(const GemmParams& p, int n_sm, int dev, cudaStream
     const unsigned grid = (unsigned)(cluster * (p.n_tiles < units ? p.n_tiles : units));
     return launch_pdl_cluster(pair_gemm_kernel<CG, EPI, MODE>, grid, THREADS, SMEM, cluster, st, p);
 }
-// Clusters of c CTAs (2 .. 8) that run at one time on the current device: they must lie within one GPC each, so it is fewer than the SMs
-// would hold.  0 where the device cannot tell.
-template <Epilogue EPI>
-inline int clusters_at_once(int c, int dev)
+// Clusters of c CTAs (2 .. 8), one CTA per SM, that are counted on to run at one time: a cluster must lie within one GPC, so it is fewer than the
+// SMs would hold.  cudaOccupancyMaxActiveClusters says 74, 45, 33, 26, 22, 15, 15 on a GPU of 148 SMs (key_compress.cuh saw 14 of 8 on
+// another); one less is counted on, as GPUs differ in which SMs they have.  Where they do not all fit, the call takes a second round.
+inline int clusters_at_once(int c, int n_sm)
 {
-    static std::atomic<int> cached[MAX_DEVICES][9];           // value + 1; 0: not asked yet
-    const int known = cached[dev][c].load(std::memory_order_relaxed);
-    if (known) return known - 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(8 * c);
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = SMEM;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)c;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaFuncSetAttribute(pair_gemm_kernel<1, EPI, SPLIT_TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess ||
-        cudaOccupancyMaxActiveClusters(&n, pair_gemm_kernel<1, EPI, SPLIT_TILES>, &cfg) != cudaSuccess) {
-        cudaGetLastError();
-        n = 0;
-    }
-    cached[dev][c].store(n + 1, std::memory_order_relaxed);
-    return n;
+    constexpr int of_148[9] = {0, 0, 73, 44, 32, 25, 21, 14, 14};
+    return of_148[c] * n_sm / 148;
 }
 
+struct Launch {
+    int cg;                         // 1 or 2
+    Mode mode;
+    int cluster;                    // CTAs per cluster (SPLIT_TILES; otherwise cg)
+};
+constexpr Launch SINGLE = {1, TILES, 1};              // what needs no cluster
+// false, and nothing enqueued, where the device refuses it (no cluster can be placed on a partitioned one: the caller goes on with SINGLE)
 template <Epilogue EPI>
-inline gf_status_t launch(int cg, const GemmParams& p, cudaStream_t st, std::atomic<uint64_t>* launches, Mode mode = TILES)
+inline bool launch(const Launch& l, const GemmParams& p, cudaStream_t st, std::atomic<uint64_t>* launches)
 {
     const int n_sm = sm_count(), dev = current_device();
-    if (n_sm < 2 || dev < 0) return GF_ERR_CUDA;
+    if (n_sm < 2 || dev < 0) return false;
     cudaError_t e = cudaErrorInvalidValue;
-    if (mode == TILES) e = cg == 2 ? launch_one<2, EPI, TILES>(p, n_sm, dev, st) : launch_one<1, EPI, TILES>(p, n_sm, dev, st);
+    if (l.mode == TILES) e = l.cg == 2 ? launch_one<2, EPI, TILES>(p, n_sm, dev, st) : launch_one<1, EPI, TILES>(p, n_sm, dev, st);
     if constexpr (EPI == EPI_GATE || EPI == EPI_GATE_GRAD)
-        if (mode == WIDE_TILES) e = launch_one<2, EPI, WIDE_TILES>(p, n_sm, dev, st);
+        if (l.mode == WIDE_TILES) e = launch_one<2, EPI, WIDE_TILES>(p, n_sm, dev, st);
+    if constexpr (EPI == EPI_GATE)
+        if (l.mode == SPLIT_TILES) e = launch_one<1, EPI, SPLIT_TILES>(p, n_sm, dev, st, l.cluster);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
     launches->fetch_add(1, std::memory_order_relaxed);
-    return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
+    return true;
 }
 
 // ---------------------------------------------------------------- several products in one launch (a gradient's)
@@ -1059,37 +1053,48 @@ __global__ void __launch_bounds__(256) sum_slices_kernel(const SumJobs jobs)
     }
 }
 
+inline void whole_tiles(Plan& plan)
+{
+    const Plan was = plan;
+    plan = Plan{1, {1, 1, 1, 1}, {}, was.bytes};      // (sums that are kept over several launches lie at the workspace's start in every plan)
+}
 // The products' launch and, where any is cut, the one that adds its slices up.  p.in holds the segments' maps; the first product may be a part
-// of a sum over several calls (its slices stay in the workspace between them).
-inline gf_status_t run_products(GemmParams& p, const Product* q, int n, const Plan& plan, Part part, void* ws, cudaStream_t st, std::atomic<uint64_t>* launches)
+// of a sum over several calls (its slices stay in the workspace between them).  Where the device places no pairs of CTAs, the plan becomes
+// one of single CTAs.
+inline gf_status_t run_products(GemmParams& p, const Product* q, int n, Plan& plan, Part part, void* ws, cudaStream_t st, std::atomic<uint64_t>* launches)
 {
     SumJobs jobs = {};
-    int order[MAX_GROUPS], depth[MAX_GROUPS];
-    for (int i = 0; i < n; ++i) {                     // the deepest tiles first: the round that ends unevenly is the shorter ones'
-        depth[i] = (int)ceil_div(q[i].steps(), plan.slices[i]);
-        int at = i;
-        while (at > 0 && depth[order[at - 1]] < depth[i]) { order[at] = order[at - 1]; --at; }
-        order[at] = i;
+    for (;;) {
+        int order[MAX_GROUPS], depth[MAX_GROUPS];
+        for (int i = 0; i < n; ++i) {                 // the deepest tiles first: the round that ends unevenly is the shorter ones'
+            depth[i] = (int)ceil_div(q[i].steps(), plan.slices[i]);
+            int at = i;
+            while (at > 0 && depth[order[at - 1]] < depth[i]) { order[at] = order[at - 1]; --at; }
+            order[at] = i;
+        }
+        p.n_groups = p.n_tiles = jobs.n = 0;
+        for (int k = 0; k < n; ++k) {
+            const int i = order[k];
+            const Product& r = q[i];
+            const Part role = i == 0 ? part : PART_ONLY;
+            const bool cut = plan.slices[i] > 1;
+            Group g = make_group(plan.cg, r.m, r.n, 128 * plan.cg);
+            for (int j = 0; j < r.n_seg; ++j) add_segment(g, r.seg[j]);
+            g.slices = plan.slices[i] < g.steps ? plan.slices[i] : g.steps;      // (a last piece may have fewer steps than slices: the rest keep their sums)
+            g.out = (unsigned char)i;
+            float* sums = reinterpret_cast<float*>(static_cast<char*>(ws) + plan.sums_at[i]);
+            g.part = sums;
+            g.mode = role == PART_ONLY ? (cut ? OUT_F32 : OUT_BF16) : role == PART_FIRST ? OUT_F32 : role == PART_MIDDLE || cut ? OUT_F32_ADD : OUT_BF16_ADD;
+            const bool f32 = g.mode == OUT_F32 || g.mode == OUT_F32_ADD;
+            if (!(f32 ? make_map_f32(&p.out[i], sums, plan.slices[i], r.m, r.n) : out_map(&p.out[i], r.out, r.m, r.n))) return GF_ERR_CUDA;
+            if (cut && (role == PART_ONLY || role == PART_LAST)) jobs.job[jobs.n++] = SumJob{sums, r.out, r.m * r.n, plan.slices[i]};
+            add_group(p, g);
+        }
+        if (launch<EPI_STORE>(Launch{plan.cg, TILES, plan.cg}, p, st, launches)) break;
+        if (plan.cg == 1 || part == PART_MIDDLE || part == PART_LAST) return GF_ERR_CUDA;
+        whole_tiles(plan);
     }
-    for (int k = 0; k < n; ++k) {
-        const int i = order[k];
-        const Product& r = q[i];
-        const Part role = i == 0 ? part : PART_ONLY;
-        const bool cut = plan.slices[i] > 1;
-        Group g = make_group(plan.cg, r.m, r.n, 128 * plan.cg);
-        for (int j = 0; j < r.n_seg; ++j) add_segment(g, r.seg[j]);
-        g.slices = plan.slices[i] < g.steps ? plan.slices[i] : g.steps;      // (a last piece may have fewer steps than slices: the rest keep their sums)
-        g.out = (unsigned char)i;
-        float* sums = reinterpret_cast<float*>(static_cast<char*>(ws) + plan.sums_at[i]);
-        g.part = sums;
-        g.mode = role == PART_ONLY ? (cut ? OUT_F32 : OUT_BF16) : role == PART_FIRST ? OUT_F32 : role == PART_MIDDLE || cut ? OUT_F32_ADD : OUT_BF16_ADD;
-        const bool f32 = g.mode == OUT_F32 || g.mode == OUT_F32_ADD;
-        if (!(f32 ? make_map_f32(&p.out[i], sums, plan.slices[i], r.m, r.n) : out_map(&p.out[i], r.out, r.m, r.n))) return GF_ERR_CUDA;
-        if (cut && (role == PART_ONLY || role == PART_LAST)) jobs.job[jobs.n++] = SumJob{sums, r.out, r.m * r.n, plan.slices[i]};
-        add_group(p, g);
-    }
-    const gf_status_t s = launch<EPI_STORE>(plan.cg, p, st, launches);
-    if (s != GF_OK || jobs.n == 0) return s;
+    if (jobs.n == 0) return GF_OK;
     long long most = 0;
     for (int i = 0; i < jobs.n; ++i) most = jobs.job[i].n > most ? jobs.job[i].n : most;
     const long long blocks = ceil_div(most, 2048), cap = 8LL * sm_count();

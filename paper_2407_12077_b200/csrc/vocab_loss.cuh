@@ -69,6 +69,15 @@ inline int forward_cg(long long rows, long long cols, int n_sm)
     return choose_cg(ceil_div(rows, 256) * ceil_div(cols, 256), ceil_div(rows, 128) * ceil_div(cols, 128), n_sm);
 }
 
+// The launch's one group: logits of rows x cols (maps 0: x, 1: the columns' rows of W).
+inline void logits(GemmParams& p, int cg, long long rows, int D, long long cols)
+{
+    Group g = make_group(cg, rows, cols, 128 * cg);
+    add_segment(g, segment(0, false, 1, false, D));
+    p.n_groups = p.n_tiles = 0;
+    add_group(p, g);
+}
+
 // Columns of P that the gradient holds at a time: 256 MB of them, between 1024 and the vocabulary, in equal pieces.
 inline long long piece_cols(long long rows, long long V)
 {
@@ -111,22 +120,23 @@ inline gf_status_t vocab_loss(const __nv_bfloat16* x, const __nv_bfloat16* w, co
     using namespace vl;
     const int n_sm = sm_count();
     if (n_sm < 2) return GF_ERR_CUDA;
-    const int cg = forward_cg(rows, V, n_sm);
     GemmParams p = {};
     if (!in_map(&p.in[0], x, rows, D) || !in_map(&p.in[1], w, V, D)) return GF_ERR_CUDA;
-    Group g = make_group(cg, rows, V, 128 * cg);
-    add_segment(g, segment(0, false, 1, false, D));
-    add_group(p, g);
     p.targets = targets;
     p.vocab = V;
     p.stats = static_cast<float2*>(ws);
     p.target_logit = reinterpret_cast<float*>(static_cast<char*>(ws) + vocab_stats_bytes(rows, V));
-    const gf_status_t s = launch<EPI_LSE>(cg, p, st, launches);
-    if (s != GF_OK) return s;
+    int cg = forward_cg(rows, V, n_sm);
+    logits(p, cg, rows, D, V);
+    if (!launch<EPI_LSE>(Launch{cg, TILES, cg}, p, st, launches)) {
+        if (cg == 1) return GF_ERR_CUDA;
+        logits(p, cg = 1, rows, D, V);
+        if (!launch<EPI_LSE>(SINGLE, p, st, launches)) return GF_ERR_CUDA;
+    }
     auto join = rows >= 1024 ? join_kernel<32> : rows >= 256 ? join_kernel<8> : join_kernel<1>;
     const int block_rows = rows >= 1024 ? 32 : rows >= 256 ? 8 : 1;
     const cudaError_t e = launch_pdl(join, (unsigned)ceil_div(rows, block_rows), JOIN_THREADS, 0, st, (const float2*)p.stats, (const float*)p.target_logit, targets, V,
-                                     2 * g.tiles_n, (int)rows, loss, lse);
+                                     2 * p.g[0].tiles_n, (int)rows, loss, lse);
     launches->fetch_add(1, std::memory_order_relaxed);
     return e == cudaSuccess ? GF_OK : GF_ERR_CUDA;
 }
@@ -139,7 +149,7 @@ inline gf_status_t vocab_loss_backward(const __nv_bfloat16* x, const __nv_bfloat
     const int n_sm = sm_count();
     if (n_sm < 2) return GF_ERR_CUDA;
     const long long step = piece_cols(rows, V);
-    const Plan plan = gradient_plan(rows, D, V);
+    Plan plan = gradient_plan(rows, D, V);
     __nv_bfloat16* P = static_cast<__nv_bfloat16*>(ws);
     for (long long v0 = 0; v0 < V; v0 += step) {
         const long long cols = V - v0 < step ? V - v0 : step;
@@ -147,18 +157,19 @@ inline gf_status_t vocab_loss_backward(const __nv_bfloat16* x, const __nv_bfloat
         const __nv_bfloat16* wp = w + (size_t)v0 * D;
         {
             GemmParams p = {};
-            const int cg = forward_cg(rows, cols, n_sm);
             if (!in_map(&p.in[0], x, rows, D) || !in_map(&p.in[1], wp, cols, D) || !out_map(&p.out[0], P, rows, pitch)) return GF_ERR_CUDA;
-            Group g = make_group(cg, rows, cols, 128 * cg);
-            add_segment(g, segment(0, false, 1, false, D));
-            add_group(p, g);
             p.targets = targets;
             p.vocab = V;
             p.first_col = (int)v0;
             p.lse = lse;
             p.dloss = dloss;
-            const gf_status_t s = launch<EPI_PROB>(cg, p, st, launches);
-            if (s != GF_OK) return s;
+            const int cg = forward_cg(rows, cols, n_sm);
+            logits(p, cg, rows, D, cols);
+            if (!launch<EPI_PROB>(Launch{cg, TILES, cg}, p, st, launches)) {
+                if (cg == 1) return GF_ERR_CUDA;
+                logits(p, 1, rows, D, cols);
+                if (!launch<EPI_PROB>(SINGLE, p, st, launches)) return GF_ERR_CUDA;
+            }
         }
         GemmParams p = {};
         const bool first = v0 == 0, last = v0 + step >= V;
