@@ -496,7 +496,8 @@ GF_API size_t gf_gated_linear_backward_workspace_bytes(long long rows, int K1, i
  *     z = x W^T,   lse = log sum_v exp(z[v]),   loss = lse - z[target].
  *   x        DEVICE bf16 [rows][D]      w  DEVICE bf16 [V][D] row-major (one row per entry of the vocabulary)
  *   targets  DEVICE int64 [rows]; one outside 0 .. V-1 means that the row has none: its loss is 0
- *   loss, lse  DEVICE fp32 [rows], written (lse is what the gradient takes)
+ *   loss, lse  DEVICE fp32 [rows], written (lse is what the gradient takes); these and targets need only their own type's alignment
+ *              (the labels of next tokens are the tokens from the second one on)
  *   workspace  DEVICE, gf_vocab_loss_workspace_bytes(rows,V) bytes, 16-byte aligned; GF_ERR_WORKSPACE if absent or too small
  * bf16 operands on the tensor cores, fp32 logits and sums of exponentials of differences to a running maximum.  D is a multiple of 8
  * (GF_ERR_UNSUPPORTED otherwise), V any positive number.  An infinite or NaN logit has the effect it has in the formula.
@@ -508,7 +509,7 @@ GF_API size_t gf_vocab_loss_workspace_bytes(long long rows, long long V);
 
 /* Gradient of gf_vocab_loss: with P[t][v] = (exp(z[t][v] - lse[t]) - [v is the target of t]) dloss[t], and 0 in rows without a
  * target,    dx = P W,   dw = P^T x.
- *   x, w, targets, sizes   as for gf_vocab_loss, lse what it wrote;   dloss  DEVICE fp32 [rows], or NULL for 1 in every row
+ *   x, w, targets, sizes   as for gf_vocab_loss, lse what it wrote;   dloss  DEVICE fp32 [rows] (alignment as lse), or NULL for 1 in every row
  *   dx [rows][D], dw [V][D]   DEVICE bf16, written; neither may be an input
  *   workspace  DEVICE, gf_vocab_loss_backward_workspace_bytes(rows,D,V) bytes, 16-byte aligned; GF_ERR_WORKSPACE if absent or
  *              too small (256 MB for a piece of P, 2 KB per row at least; fp32 sums of dx where the vocabulary takes several pieces, and of

@@ -671,7 +671,8 @@ def layernorm_heads_backward(y, dout, gamma=None, eps=1e-5, want_params=True, dy
     dt, f32 = y.dtype, torch.float32
     sfx = _suffix(dt)
     _one_device(y=y, dout=dout, gamma=gamma, dy=dy, workspace=workspace)
-    ins = [_dev(y, "y"), _dev(None if gamma is None else gamma.reshape(D), "gamma", f32), float(eps), _dev(dout, "dout", dt, y.shape)]
+    gamma = None if gamma is None else gamma.reshape(D)       # (a copy, where it is one, lives until the call)
+    ins = [_dev(y, "y"), _dev(gamma, "gamma", f32), float(eps), _dev(dout, "dout", dt, y.shape)]
     if dy is None:
         dy = torch.empty_like(y)
     dgamma = dbeta = ws = None

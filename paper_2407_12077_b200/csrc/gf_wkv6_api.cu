@@ -47,7 +47,7 @@ float* static_scratch()
     return addr[dev];
 }
 
-inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+inline bool misaligned(const void* p, unsigned to = 16) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
 // Pointer checks shared by all compute calls; `need_state_in` is false where NULL means zero.
 gf_status_t check_ptrs(const void* r, const void* k, const void* v, const void* x, const float* u,
@@ -215,7 +215,7 @@ gf_status_t check_vocab(const void* x, const void* w, const void* targets, long 
     if (D == 0 || (D & 7)) return GF_ERR_UNSUPPORTED;
     if (rows >= (1LL << 31) - 256 || V >= (1LL << 31) - 256 || (rows / 128 + 1) * (V / 128 + 1) >= 1LL << 30) return GF_ERR_UNSUPPORTED;
     if ((rows / 128 + V / 128 + 2) * (D / 128 + 1) >= 1LL << 30) return GF_ERR_UNSUPPORTED;
-    if (!x || !w || !targets || misaligned(x) || misaligned(w) || misaligned(targets)) return GF_ERR_INVALID_ARG;
+    if (!x || !w || !targets || misaligned(x) || misaligned(w) || misaligned(targets, 8)) return GF_ERR_INVALID_ARG;
     return GF_OK;
 }
 gf_status_t zeros(void* p, size_t bytes, cudaStream_t st) { return cudaMemsetAsync(p, 0, bytes, st) == cudaSuccess ? GF_OK : GF_ERR_CUDA; }
@@ -953,7 +953,7 @@ gf_status_t gf_vocab_loss(const void* x, const void* w, const int64_t* targets, 
     using bf = __nv_bfloat16;
     const gf_status_t e = check_vocab(x, w, targets, rows, D, V);
     if (e != GF_OK || rows == 0) return e;
-    if (!loss || !lse || loss == lse || misaligned(loss) || misaligned(lse) || misaligned(workspace)) return GF_ERR_INVALID_ARG;
+    if (!loss || !lse || loss == lse || misaligned(loss, 4) || misaligned(lse, 4) || misaligned(workspace)) return GF_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < gf::vocab_loss_bytes(rows, V)) return GF_ERR_WORKSPACE;
     return gf::vocab_loss((const bf*)x, (const bf*)w, (const long long*)targets, loss, lse, rows, D, V, workspace, (cudaStream_t)stream, &g_launches);
 }
@@ -966,7 +966,7 @@ gf_status_t gf_vocab_loss_backward(const void* x, const void* w, const int64_t* 
     if (e != GF_OK) return e;
     if (rows == 0) return dw && D > 0 ? zeros(dw, (size_t)V * D * 2, (cudaStream_t)stream) : GF_OK;
     if (!lse || !dx || !dw || dx == dw || dx == x || dx == w || dw == x || dw == w) return GF_ERR_INVALID_ARG;
-    if (misaligned(lse) || misaligned(dloss) || misaligned(dx) || misaligned(dw) || misaligned(workspace)) return GF_ERR_INVALID_ARG;
+    if (misaligned(lse, 4) || misaligned(dloss, 4) || misaligned(dx) || misaligned(dw) || misaligned(workspace)) return GF_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < gf::vocab_loss_backward_bytes(rows, D, V)) return GF_ERR_WORKSPACE;
     return gf::vocab_loss_backward((const bf*)x, (const bf*)w, (const long long*)targets, lse, dloss, (bf*)dx, (bf*)dw, rows, D, V, workspace,
                                    (cudaStream_t)stream, &g_launches);

@@ -256,9 +256,9 @@ __device__ __forceinline__ Tile tile_at(const GemmParams& p, int tile, int share
     int i = tile - g.first;
     t.slice = i / places;
     i -= t.slice * places;
-    const int of = g.slices * shares, nth = t.slice + share;
-    t.lo = g.steps * nth / of;                        // (steps < 2^25, of <= 32)
-    t.hi = g.steps * (nth + 1) / of;
+    const uint32_t of = g.slices * shares, nth = t.slice + share;
+    t.lo = (int)((uint32_t)g.steps * nth / of);       // (steps <= 2^26, of <= 32)
+    t.hi = (int)((uint32_t)g.steps * (nth + 1) / of);
     // bands of eight tiles along m, column by column: the tiles that run at one time share few rows of A and of B
     const int per = 8 * g.tiles_n, band = i / per, rest = i - band * per;
     const int h = min(8, g.tiles_m - 8 * band);
@@ -483,17 +483,17 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
             const bool in = row < g.rows;
             // what the epilogue reads from memory is under way while the products run
             const int width = EPI == EPI_GATE || EPI == EPI_GATE_GRAD ? (WIDE || p.gated ? HW : BN) : BN;
-            constexpr int DY_BLOCKS = EPI == EPI_GATE_GRAD ? (BN + 127) / 128 : 1;      // blocks of 64 columns that a warp takes
-            uint32_t dy[DY_BLOCKS][2][16];
-            if constexpr (EPI == EPI_GATE_GRAD) {
-#pragma unroll
-                for (int k = 0; k < DY_BLOCKS; ++k)
+            uint32_t dy[2][16];                       // of the warp's first block of 64 columns
+            auto load_dy = [&](int c) {
+                if constexpr (EPI == EPI_GATE_GRAD) {
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const int c = 64 * part + 128 * k + 32 * half, col = tn * width + c;
-                        load_row32(p.dy + (size_t)row * g.cols + col, in && c < width, g.cols - col, dy[k][half]);
+                        const int col = tn * width + c + 32 * half;
+                        load_row32(p.dy + (size_t)row * g.cols + col, in && c < width, g.cols - col, dy[half]);
                     }
-            }
+                }
+            };
+            load_dy(64 * part);
             long long target = -1;                    // (-1: none)
             float lse = 0.f, weight = 0.f;
             if constexpr (EPI == EPI_LSE || EPI == EPI_PROB) {
@@ -612,14 +612,14 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                 }
             } else if constexpr (EPI == EPI_GATE_GRAD && WIDE) {
                 // db needs the first product alone: it leaves, and dy act'(a) takes the first product's place, while the second one runs
-#pragma unroll
-                for (int k = 0; k < DY_BLOCKS; ++k) {
-                    const int c = 64 * part + 128 * k, col = tn * HW + c;
+                for (int c = 64 * part; c < HW; c += 128) {
+                    const int col = tn * HW + c;
                     if (col >= g.cols) break;
+                    if (c >= 128) load_dy(c);
                     take_slab();
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const uint32_t(&d)[16] = dy[k][half];
+                        const uint32_t(&d)[16] = dy[half];
                         float a[32], b[32];
                         ld_acc(acc + c + 32 * half, a);
                         by_act(p.act, [&](auto k) {
@@ -677,15 +677,15 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                     send(&p.out[0], col);
                 }
             } else if constexpr (EPI == EPI_GATE_GRAD) {
-#pragma unroll
-                for (int k = 0; k < DY_BLOCKS; ++k) {
-                    const int c = 64 * part + 128 * k, col = tn * width + c;
-                    if (c >= width || col >= g.cols) break;
+                for (int c = 64 * part; c < width; c += 128) {
+                    const int col = tn * width + c;
+                    if (col >= g.cols) break;
+                    if (c >= 128) load_dy(c);
                     take_slab();
                     uint32_t later[2][16];            // db, in bf16, until da has left the slab
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const uint32_t(&d)[16] = dy[k][half];
+                        const uint32_t(&d)[16] = dy[half];
                         float a[32];
                         ld_acc(acc + c + 32 * half, a);
                         if (p.gated) {
@@ -779,6 +779,10 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                             const float2 o = mul2(make_float2(v[j], v[j + 1]), make_float2(weight, weight));
                             v[j] = o.x;
                             v[j + 1] = o.y;
+                        }
+                        if (__any_sync(0xffffffffu, target < 0)) {    // (zero, whatever the logits of a row without a target are)
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] = target < 0 ? 0.f : v[j];
                         }
                         if (col + 32 * half + 32 > g.cols) {          // (columns that fill up a row of the tensor: an operand, so zero)
 #pragma unroll

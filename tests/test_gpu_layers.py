@@ -104,6 +104,16 @@ def test_norm_gradient_in_place_without_gamma_and_without_sums(dtype):
     assert torch.equal(got[0], want[0]) and got[1] is None and got[2] is None
 
 
+def test_norm_gradient_with_a_gamma_that_has_to_be_copied():
+    g = torch.Generator().manual_seed(8)
+    y, dout, wide = dev(normal(g, 50, 4, 64), normal(g, 50, 4, 64), torch.randn(4, 128, generator=g))
+    gamma = wide[:, :64]
+    want = gf.layernorm_heads_backward(y, dout, gamma.contiguous())
+    for _ in range(3):
+        got = gf.layernorm_heads_backward(y, dout, gamma)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_norm_gradient_of_a_constant_row_and_of_no_rows():
     y, dout = torch.full((2, 4, 64), 3.0, device=DEV), torch.ones(2, 4, 64, device=DEV)
     dy, dg, db = gf.layernorm_heads_backward(y, dout, None, 1e-5)       # deviations and the centred gradient are exactly zero
@@ -368,6 +378,29 @@ def test_vocab_loss_of_large_and_infinite_logits_and_of_nothing():
     loss, lse = gf.vocab_loss(none, wd, no_t)
     dx, dw = gf.vocab_loss_backward(none, wd, no_t, lse)
     assert loss.shape == lse.shape == (0,) and dx.shape == (0, D) and not dw.any()
+
+
+def test_vocab_loss_of_next_tokens_and_rows_without_a_target():
+    """Labels that are the tokens from the second one on (aligned to 8 bytes only), losses' weights that start anywhere, and a row without a
+    target whose logits overflow: nothing of it reaches the gradients."""
+    g = torch.Generator().manual_seed(6)
+    ids = torch.randint(0, 300, (129,), generator=g).to(DEV)
+    x, w = dev(normal(g, 129, 64), normal(g, 300, 64))
+    d = torch.randn(130, generator=g).to(DEV)
+    got = gf.vocab_loss(x[:-1], w, ids[1:])
+    want = gf.vocab_loss(x[:-1], w, ids[1:].clone())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    lse = torch.cat([torch.zeros(1, device=DEV), got[1]])[1:]
+    a, b = gf.vocab_loss_backward(x[:-1], w, ids[1:], lse, d[1:129]), gf.vocab_loss_backward(x[:-1], w, ids[1:].clone(), got[1], d[1:129].clone())
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    t = ids.clone()
+    t[5] = -100
+    loss, lse = gf.vocab_loss(x, w, t)
+    clean = gf.vocab_loss_backward(x, w, t, lse)
+    lse[5] = float("nan")
+    got = gf.vocab_loss_backward(x, w, t, lse)
+    gf.last_device_status()
+    assert all(torch.equal(p, q) for p, q in zip(got, clean)) and not got[0][5].any()
 
 
 # ------------------------------------------------------------------------------------------------ as they are used together
