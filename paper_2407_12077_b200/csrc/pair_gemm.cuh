@@ -35,7 +35,6 @@ namespace pg {
 
 using namespace ck;                                   // PTX wrappers, descriptors, TILE, bounded waits
 using kc::cluster_sync;
-using kc::tmem_ld_row32;
 
 constexpr int N_EPI = 8;                              // epilogue warps: two per tensor-memory sub-partition
 constexpr int THREADS = 64 + 32 * N_EPI;
@@ -233,12 +232,46 @@ __device__ __forceinline__ void put_bf16(uint32_t slab, int lane, int half, cons
         sts128(slab + swz(lane, (4 * half + q) << 4), pack_bf16(o[8 * q], o[8 * q + 1]), pack_bf16(o[8 * q + 2], o[8 * q + 3]),
                pack_bf16(o[8 * q + 4], o[8 * q + 5]), pack_bf16(o[8 * q + 6], o[8 * q + 7]));
 }
+// 32 columns of the lane's accumulator row
 __device__ __forceinline__ void ld_acc(uint32_t taddr, float (&o)[32])
 {
-    uint32_t v[32];
-    tmem_ld_row32(taddr, v);
-#pragma unroll
-    for (int j = 0; j < 32; ++j) o[j] = __uint_as_float(v[j]);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+        "%0, %1, %2, %3, %4, %5, %6, %7, "
+        "%8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, "
+        "%24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(o[0]), "=f"(o[1]), "=f"(o[2]), "=f"(o[3]), "=f"(o[4]), "=f"(o[5]), "=f"(o[6]), "=f"(o[7]),
+          "=f"(o[8]), "=f"(o[9]), "=f"(o[10]), "=f"(o[11]), "=f"(o[12]), "=f"(o[13]), "=f"(o[14]), "=f"(o[15]),
+          "=f"(o[16]), "=f"(o[17]), "=f"(o[18]), "=f"(o[19]), "=f"(o[20]), "=f"(o[21]), "=f"(o[22]), "=f"(o[23]),
+          "=f"(o[24]), "=f"(o[25]), "=f"(o[26]), "=f"(o[27]), "=f"(o[28]), "=f"(o[29]), "=f"(o[30]), "=f"(o[31])
+        : "r"(taddr) : "memory");
+}
+// two runs of 32 columns with one wait
+__device__ __forceinline__ void ld_acc2(uint32_t t0, float (&a)[32], uint32_t t1, float (&b)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+        "%0, %1, %2, %3, %4, %5, %6, %7, "
+        "%8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, "
+        "%24, %25, %26, %27, %28, %29, %30, %31}, [%64];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+        "%32, %33, %34, %35, %36, %37, %38, %39, "
+        "%40, %41, %42, %43, %44, %45, %46, %47, "
+        "%48, %49, %50, %51, %52, %53, %54, %55, "
+        "%56, %57, %58, %59, %60, %61, %62, %63}, [%65];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(a[0]), "=f"(a[1]), "=f"(a[2]), "=f"(a[3]), "=f"(a[4]), "=f"(a[5]), "=f"(a[6]), "=f"(a[7]),
+          "=f"(a[8]), "=f"(a[9]), "=f"(a[10]), "=f"(a[11]), "=f"(a[12]), "=f"(a[13]), "=f"(a[14]), "=f"(a[15]),
+          "=f"(a[16]), "=f"(a[17]), "=f"(a[18]), "=f"(a[19]), "=f"(a[20]), "=f"(a[21]), "=f"(a[22]), "=f"(a[23]),
+          "=f"(a[24]), "=f"(a[25]), "=f"(a[26]), "=f"(a[27]), "=f"(a[28]), "=f"(a[29]), "=f"(a[30]), "=f"(a[31]),
+          "=f"(b[0]), "=f"(b[1]), "=f"(b[2]), "=f"(b[3]), "=f"(b[4]), "=f"(b[5]), "=f"(b[6]), "=f"(b[7]),
+          "=f"(b[8]), "=f"(b[9]), "=f"(b[10]), "=f"(b[11]), "=f"(b[12]), "=f"(b[13]), "=f"(b[14]), "=f"(b[15]),
+          "=f"(b[16]), "=f"(b[17]), "=f"(b[18]), "=f"(b[19]), "=f"(b[20]), "=f"(b[21]), "=f"(b[22]), "=f"(b[23]),
+          "=f"(b[24]), "=f"(b[25]), "=f"(b[26]), "=f"(b[27]), "=f"(b[28]), "=f"(b[29]), "=f"(b[30]), "=f"(b[31])
+        : "r"(t0), "r"(t1) : "memory");
 }
 
 struct Tile {
@@ -545,11 +578,12 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                             }
                         }
                     } else {
+                        float w[2][32];
+                        ld_acc2(acc + c, w[0], acc + c + 32, w[1]);
                         take_slab();
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
-                            float v[32];
-                            ld_acc(acc + c + 32 * half, v);
+                            float(&v)[32] = w[half];
                             if (g.mode == OUT_BF16_ADD && in) {
                                 const float* src = g.part + (size_t)row * g.cols + col + 32 * half;
 #pragma unroll
@@ -602,8 +636,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         float a[32], b[32];
-                        ld_acc(acc + c + 32 * half, a);
-                        ld_acc(acc + HW + c + 32 * half, b);
+                        ld_acc2(acc + c + 32 * half, a, acc + HW + c + 32 * half, b);
 #pragma unroll
                         for (int j = 0; j < 32; ++j) a[j] *= b[j];
                         put_bf16(sl, lane, half, a);
@@ -645,8 +678,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         float a[32], b[32];
-                        ld_acc(acc + c + 32 * half, a);
-                        ld_acc(acc + HW + c + 32 * half, b);
+                        ld_acc2(acc + c + 32 * half, a, acc + HW + c + 32 * half, b);
 #pragma unroll
                         for (int j = 0; j < 32; ++j) a[j] *= b[j];
                         put_bf16(sl, lane, half, a);
@@ -660,15 +692,14 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                     take_slab();
 #pragma unroll 1                                      // (a small call runs this code once: what it fetches of it counts)
                     for (int half = 0; half < 2; ++half) {
-                        float a[32];
-                        ld_acc(acc + c + 32 * half, a);
+                        float a[32], b[32];
+                        if (p.gated) ld_acc2(acc + c + 32 * half, a, acc + HW + c + 32 * half, b);
+                        else ld_acc(acc + c + 32 * half, a);
                         by_act(p.act, [&](auto k) {
 #pragma unroll
                             for (int j = 0; j < 32; ++j) a[j] = act_value<decltype(k)::value>(a[j]);
                         });
                         if (p.gated) {
-                            float b[32];
-                            ld_acc(acc + HW + c + 32 * half, b);
 #pragma unroll
                             for (int j = 0; j < 32; ++j) a[j] *= b[j];
                         }
@@ -687,10 +718,9 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                     for (int half = 0; half < 2; ++half) {
                         const uint32_t(&d)[16] = dy[half];
                         float a[32];
-                        ld_acc(acc + c + 32 * half, a);
                         if (p.gated) {
                             float b[32];
-                            ld_acc(acc + HW + c + 32 * half, b);
+                            ld_acc2(acc + c + 32 * half, a, acc + HW + c + 32 * half, b);
                             by_act(p.act, [&](auto k) {
 #pragma unroll
                                 for (int j = 0; j < 32; ++j) {
@@ -703,6 +733,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
 #pragma unroll
                             for (int j = 0; j < 16; ++j) later[half][j] = pack_bf16(b[2 * j], b[2 * j + 1]);
                         } else {
+                            ld_acc(acc + c + 32 * half, a);
                             by_act(p.act, [&](auto k) {
 #pragma unroll
                                 for (int j = 0; j < 32; ++j) {
@@ -727,34 +758,41 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                 // a warp takes half of the tile's columns.  exp is taken of differences to a reference, the largest value so far (0
                 // instead of an infinite one: the sum is then infinite, or zero, by itself); a NaN reaches the sum through its own exponential
                 float ref = -FLT_MAX, sum = 0.f;
-                for (int c = HW * part; c < HW * part + HW; c += 32) {
+                for (int c = HW * part; c < HW * part + HW; c += 64) {
                     const int col = tn * BN + c;
                     if (col >= g.cols) break;
-                    float v[32];
-                    ld_acc(acc + c, v);
-                    if (col + 32 > g.cols) {
+                    float v[2][32];
+                    ld_acc2(acc + c, v[0], acc + c + 32, v[1]);
+                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (col + j >= g.cols) v[j] = -INFINITY;
+                    for (int half = 0; half < 2; ++half) {
+                        if (col + 32 * half + 32 > g.cols) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (col + 32 * half + j >= g.cols) v[half][j] = -INFINITY;
+                        }
+                        const uint32_t hit = one_of_32(target - (col + 32 * half));
+                        if (__any_sync(0xffffffffu, hit)) {
+                            float z = 0.f;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) z = hit >> j & 1 ? v[half][j] : z;
+                            if (hit) p.target_logit[row] = z;
+                        }
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) t4[j & 3] = fmaxf(t4[j & 3], v[half][j]);
                     }
-                    const uint32_t hit = one_of_32(target - col);
-                    if (__any_sync(0xffffffffu, hit)) {
-                        float z = 0.f;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) z = hit >> j & 1 ? v[j] : z;
-                        if (hit) p.target_logit[row] = z;
-                    }
-                    float t4[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-                    for (int j = 4; j < 32; ++j) t4[j & 3] = fmaxf(t4[j & 3], v[j]);
                     float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
                     top = c == HW * part ? top : fmaxf(top, ref);
                     top = fabsf(top) < INFINITY ? top : 0.f;
-                    float2 s2[2] = {make_float2(sum * ex2((ref - top) * LOG2E), 0.f), make_float2(0.f, 0.f)};
-                    exp_of_difference(v, top);
+                    float2 s2[4] = {make_float2(sum * ex2((ref - top) * LOG2E), 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) s2[j & 1] = add2(s2[j & 1], make_float2(v[2 * j], v[2 * j + 1]));
-                    sum = (s2[0].x + s2[0].y) + (s2[1].x + s2[1].y);
+                    for (int half = 0; half < 2; ++half) {
+                        exp_of_difference(v[half], top);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) s2[j & 3] = add2(s2[j & 3], make_float2(v[half][2 * j], v[half][2 * j + 1]));
+                    }
+                    s2[0] = add2(add2(s2[0], s2[1]), add2(s2[2], s2[3]));
+                    sum = s2[0].x + s2[0].y;
                     ref = top;
                 }
                 if (in) p.stats[(size_t)(2 * tn + part) * g.rows + row] = make_float2(ref, sum);
@@ -763,11 +801,12 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                 for (int c = 64 * part; c < BN; c += 128) {
                     const int col = tn * BN + c;
                     if (col >= g.cols) break;
+                    float e[2][32];
+                    ld_acc2(acc + c, e[0], acc + c + 32, e[1]);
                     take_slab();
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        float v[32];
-                        ld_acc(acc + c + 32 * half, v);
+                        float(&v)[32] = e[half];
                         exp_of_difference(v, lse);
                         const uint32_t hit = one_of_32(at - (col + 32 * half));
                         if (__any_sync(0xffffffffu, hit)) {
