@@ -19,7 +19,7 @@
 // first product alone it does while the second one runs.  SPLIT, for results of few tiles (decoding): a cluster of up to eight CTAs divides a tile's
 // contraction indices, leaves its sums in shared memory and adds them up there, each CTA a share of the tile's places.
 //
-//   warp 0      TMA producer: 64 contraction indices of A and B (16 KB each per CTA) per stage of a six-stage ring
+//   warp 0      TMA producer: 64 contraction indices of A and B (16 KB each per CTA) per stage of a five-stage ring
 //   warp 1      tensor-memory allocation; an elected lane of the leading CTA issues the four products of a stage
 //   warps 2-9   epilogue: a lane owns a row of the tile, 32 columns at a time, two warps sharing a row's columns out in blocks of 64
 // Every wait is bounded (status flag and abort as in the prefill kernel); a pair's CTAs meet before either leaves.
@@ -38,10 +38,10 @@ using kc::cluster_sync;
 
 constexpr int N_EPI = 8;                              // epilogue warps: two per tensor-memory sub-partition
 constexpr int THREADS = 64 + 32 * N_EPI;
-constexpr int NSTAGE = 6;
+constexpr int NSTAGE = 5;
 constexpr int STAGE_BYTES = 4 * TILE;                 // 128 x 64 of A, 128 x 64 of B
-constexpr int OFF_SLAB = NSTAGE * STAGE_BYTES;        // [N_EPI warps][32 rows x 128 B]
-constexpr int OFF_MISC = OFF_SLAB + N_EPI * 4096;     // abort word, wait limit, tensor-memory address, barriers
+constexpr int OFF_SLAB = NSTAGE * STAGE_BYTES;        // [N_EPI warps][2][32 rows x 128 B]
+constexpr int OFF_MISC = OFF_SLAB + N_EPI * 2 * 4096;     // abort word, wait limit, tensor-memory address, barriers
 constexpr int SUMS_PITCH = (2 * 128 + 4) * 4;          // SPLIT_TILES: a row of both products' sums, fp32, in place of the ring
 static_assert(128 * SUMS_PITCH <= OFF_SLAB, "partial sums");
 constexpr int SMEM = OFF_MISC + 256 + 1024;           // + slack for manual 1024-byte alignment
@@ -287,15 +287,18 @@ __device__ __forceinline__ Tile tile_at(const GemmParams& p, int tile, int share
     const Group& g = p.g[t.g];
     const int places = g.tiles_m * g.tiles_n;
     int i = tile - g.first;
-    t.slice = i / places;
-    i -= t.slice * places;
+    t.slice = 0;
+    if (g.slices > 1) {
+        t.slice = i / places;
+        i -= t.slice * places;
+    }
     const uint32_t of = g.slices * shares, nth = t.slice + share;
     t.lo = (int)((uint32_t)g.steps * nth / of);       // (steps <= 2^26, of <= 32)
     t.hi = (int)((uint32_t)g.steps * (nth + 1) / of);
     // bands of eight tiles along m, column by column: the tiles that run at one time share few rows of A and of B
     const int per = 8 * g.tiles_n, band = i / per, rest = i - band * per;
     const int h = min(8, g.tiles_m - 8 * band);
-    t.n = rest / h;
+    t.n = h == 8 ? rest >> 3 : rest / h;
     t.m = 8 * band + rest - t.n * h;
     return t;
 }
@@ -506,10 +509,30 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
         // ============================== epilogue warps ==============================
         const int sp = warp & 3;                      // tensor-memory sub-partition: accumulator rows 32*sp .. 32*sp+31
         const int part = (warp - 2) >> 2;             // takes the row's blocks of 64 columns part, part + 2, ..
-        const uint32_t sl = sbase + OFF_SLAB + (warp - 2) * 4096;
+        const uint32_t slabs = sbase + OFF_SLAB + (warp - 2) * 2 * 4096;
+        uint32_t sl = slabs;                          // the slab that was filled last
+        // a row's target (-1: none), normaliser and weight, read a tile ahead
+        struct RowValues { long long target; float lse, weight; };
+        auto row_values = [&](const Tile& t) {
+            RowValues v = {-1, 0.f, 0.f};
+            if constexpr (EPI == EPI_LSE || EPI == EPI_PROB) {
+                const int r = t.m * 128 * CG + 128 * (int)rank + 32 * sp + lane;
+                if (r < p.g[t.g].rows) {
+                    v.target = p.targets[r];
+                    if (v.target < 0 || v.target >= p.vocab) v.target = -1;
+                    if constexpr (EPI == EPI_PROB) {
+                        v.lse = p.lse[r];
+                        v.weight = v.target < 0 ? 0.f : p.dloss ? p.dloss[r] : 1.f;
+                    }
+                }
+            }
+            return v;
+        };
+        Tile next = first;
+        RowValues ahead = row_values(first);
         int ti = 0;
         for (int tile = unit; tile < p.n_tiles; tile += units, ++ti) {
-            const Tile place = tile == unit ? first : tile_at(p, tile, share, shares);
+            const Tile place = next;
             const Group& g = p.g[place.g];
             const int tm = place.m, tn = place.n;
             const int row0 = tm * 128 * CG + 128 * (int)rank + 32 * sp, row = row0 + lane;
@@ -527,32 +550,27 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                 }
             };
             load_dy(64 * part);
-            long long target = -1;                    // (-1: none)
-            float lse = 0.f, weight = 0.f;
-            if constexpr (EPI == EPI_LSE || EPI == EPI_PROB) {
-                if (in) target = p.targets[row];
-                if (target < 0 || target >= p.vocab) target = -1;
-            }
-            if constexpr (EPI == EPI_PROB) {
-                if (in) {
-                    lse = p.lse[row];
-                    weight = target < 0 ? 0.f : p.dloss ? p.dloss[row] : 1.f;
-                }
-            }
+            const long long target = ahead.target;
+            const float lse = ahead.lse, weight = ahead.weight;
             const int set = SETS == 2 ? ti & 1 : 0;
             if (!mbar_wait_warp(bar(WIDE ? BAR_LEFT_FULL : BAR_ACC_FULL + set), (SETS == 2 ? ti >> 1 : ti) & 1, abort_flag)) break;
             tc_fence_after();
             const uint32_t acc = tmem + ((uint32_t)(32 * sp) << 16) + ACC_COLS * set;
-            // the slab, once no store is reading it any more
+            if (tile + units < p.n_tiles) {           // the next tile's place, and what it reads of its rows
+                next = tile_at(p, tile + units, share, shares);
+                ahead = row_values(next);
+            }
+            // the warp's other slab, once no store is reading it any more (the one before may be under way)
             auto take_slab = [&]() {
-                if (lane == 0) bulk_wait_read<0>();
+                sl ^= slabs ^ (slabs + 4096);
+                if (lane == 0) bulk_wait_read<1>();
                 __syncwarp();
             };
             auto send = [&](const CUtensorMap* m, int col) {
                 fence_proxy_async();
                 __syncwarp();
-                if (lane == 0 && row0 < g.rows) {
-                    tma_store_2d(m, col, row0, sl);
+                if (lane == 0) {                      // (a group each time, if an empty one: take_slab() counts them)
+                    if (row0 < g.rows) tma_store_2d(m, col, row0, sl);
                     bulk_commit();
                 }
             };
@@ -571,9 +589,11 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                                 sts128(sl + swz(lane, q << 4), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
                             fence_proxy_async();
                             __syncwarp();
-                            if (lane == 0 && row0 < g.rows && col + 32 * half < g.cols) {
-                                if (g.mode == OUT_F32) tma_store_3d(&p.out[g.out], col + 32 * half, row0, place.slice, sl);
-                                else tma_reduce_add_3d(&p.out[g.out], col + 32 * half, row0, place.slice, sl);
+                            if (lane == 0) {
+                                if (row0 < g.rows && col + 32 * half < g.cols) {
+                                    if (g.mode == OUT_F32) tma_store_3d(&p.out[g.out], col + 32 * half, row0, place.slice, sl);
+                                    else tma_reduce_add_3d(&p.out[g.out], col + 32 * half, row0, place.slice, sl);
+                                }
                                 bulk_commit();
                             }
                         }
