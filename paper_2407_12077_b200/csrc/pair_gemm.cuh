@@ -72,6 +72,7 @@ struct Segment {
 };
 struct Group {
     int tiles_m, tiles_n, first;    // first: number of the group's first tile in the launch
+    uint32_t per_mul, per_shift;    // division by the tiles of a band (see tile_at): (mulhi(i, per_mul) + i) >> per_shift
     int slices;                     // tiles per place of the result, each with its share of the contraction indices (all segments' in a row)
     int steps;                      // of all segments
     int n_seg;
@@ -181,10 +182,16 @@ __device__ __forceinline__ float normal_cdf(float a)
     const float q = 0.5f * t * ex2(fmaf(-x, x, p) * LOG2E);
     return a < 0.f ? q : 1.f - q;
 }
+__device__ __forceinline__ float relu(float a)        // (a NaN stays one)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(a));
+    return r;
+}
 template <int ACT> __device__ __forceinline__ float act_value(float a)
 {
     if constexpr (ACT == ACT_RELU2) {
-        const float r = a != a ? a : fmaxf(a, 0.f);
+        const float r = relu(a);
         return r * r;
     } else if constexpr (ACT == ACT_GELU) {
         return a * normal_cdf(a);
@@ -197,7 +204,7 @@ template <int ACT> __device__ __forceinline__ float act_value(float a)
 template <int ACT> __device__ __forceinline__ void act_grad(float a, float& f, float& df)
 {
     if constexpr (ACT == ACT_RELU2) {
-        const float r = a != a ? a : fmaxf(a, 0.f);
+        const float r = relu(a);
         f = r * r;
         df = 2.f * r;
     } else if constexpr (ACT == ACT_GELU) {
@@ -296,7 +303,7 @@ __device__ __forceinline__ Tile tile_at(const GemmParams& p, int tile, int share
     t.lo = (int)((uint32_t)g.steps * nth / of);       // (steps <= 2^26, of <= 32)
     t.hi = (int)((uint32_t)g.steps * (nth + 1) / of);
     // bands of eight tiles along m, column by column: the tiles that run at one time share few rows of A and of B
-    const int per = 8 * g.tiles_n, band = i / per, rest = i - band * per;
+    const int per = 8 * g.tiles_n, band = (int)((__umulhi((uint32_t)i, g.per_mul) + (uint32_t)i) >> g.per_shift), rest = i - band * per;
     const int h = min(8, g.tiles_m - 8 * band);
     t.n = h == 8 ? rest >> 3 : rest / h;
     t.m = 8 * band + rest - t.n * h;
@@ -937,6 +944,10 @@ inline Group make_group(int cg, long long rows, long long cols, int width)
     g.rows = (int)rows;
     g.cols = (int)cols;
     g.slices = 1;
+    // i / d for i < 2^30, d = 8 tiles_n: with s = ceil(log2 d), floor(2^32 (2^s - d) / d) + 1 and one addition (Granlund, Montgomery)
+    const uint64_t d = 8ull * g.tiles_n;
+    while ((1ull << g.per_shift) < d) ++g.per_shift;
+    g.per_mul = (uint32_t)((((1ull << g.per_shift) - d) << 32) / d + 1);
     return g;
 }
 inline Segment segment(int a, bool a_mn, int b, bool b_mn, long long depth, BCols cols = B_WHOLE, bool right = false)
