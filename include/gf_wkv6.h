@@ -26,6 +26,8 @@
  *     ([i][j], i = key channel).  Base pointers must be 16-byte aligned.
  *   - dtype of r,k,v,x,y: bf16 for the un-suffixed names, fp32 for the _f32 twins.
  *     u and the states are always fp32.  All accumulation is fp32.
+ *   - A `workspace` argument belongs to its call until the call's kernels have run: calls that overlap on the GPU (other streams, graphs that
+ *     are replayed side by side) need one each.
  *   - state_in == NULL means a zero initial state.  state_out == NULL skips the
  *     final-state write.  state_out may alias state_in (in-place update).  y must
  *     not overlap any input.

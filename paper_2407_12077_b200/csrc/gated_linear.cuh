@@ -31,8 +31,8 @@ inline int choose_cg(long long large, long long small, int n_sm)
 inline bool products(GemmParams& p, const Launch& l, const Shape& s, const __nv_bfloat16* x, const __nv_bfloat16* w, const __nv_bfloat16* x2, const __nv_bfloat16* w2)
 {
     const bool gated = s.K2 > 0;
-    if (!in_map(&p.in[0], x, s.rows, s.K1) || !in_map(&p.in[1], w, s.K1, s.F)) return false;
-    if (gated && (!in_map(&p.in[2], w2, s.K2, s.F) || !in_map(&p.in[3], x2, s.rows, s.K2))) return false;
+    if (!in_map(p, 0, x, s.rows, s.K1) || !in_map(p, 1, w, s.K1, s.F)) return false;
+    if (gated && (!in_map(p, 2, w2, s.K2, s.F) || !in_map(p, 3, x2, s.rows, s.K2))) return false;
     const bool whole = l.mode != TILES;               // an accumulator of a whole tile's columns for each product
     Group g = make_group(l.cg, s.rows, s.F, gated && !whole ? 64 * l.cg : 128 * l.cg);
     if (!gated || (s.same && !whole)) {
@@ -144,8 +144,8 @@ inline gf_status_t gated_linear_backward(const __nv_bfloat16* x, const __nv_bflo
     }
     if (!done) return GF_ERR_CUDA;
     GemmParams p = {};
-    if (!in_map(&p.in[0], da, s.rows, s.F) || !in_map(&p.in[2], w, s.K1, s.F) || !in_map(&p.in[4], x, s.rows, s.K1)) return GF_ERR_CUDA;
-    if (gated && (!in_map(&p.in[1], db, s.rows, s.F) || !in_map(&p.in[3], w2, s.K2, s.F) || !in_map(&p.in[5], x2, s.rows, s.K2))) return GF_ERR_CUDA;
+    if (!in_map(p, 0, da, s.rows, s.F) || !in_map(p, 2, w, s.K1, s.F) || !in_map(p, 4, x, s.rows, s.K1)) return GF_ERR_CUDA;
+    if (gated && (!in_map(p, 1, db, s.rows, s.F) || !in_map(p, 3, w2, s.K2, s.F) || !in_map(p, 5, x2, s.rows, s.K2))) return GF_ERR_CUDA;
     Product q[MAX_GROUPS];
     const int n = gradient_products(s, q, dx, dw, dx2, dw2);
     Plan plan = plan_products(q, n, plan_sms(), false);

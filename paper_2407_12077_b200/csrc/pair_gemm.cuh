@@ -87,6 +87,7 @@ struct GemmParams {
     CUtensorMap in[MAX_IN], out[MAX_OUT];
     Group g[MAX_GROUPS];
     int n_groups, n_tiles;
+    uint32_t in_used;               // bit per map of `in`
     // EPI_GATE, EPI_GATE_GRAD
     int act;
     bool gated;
@@ -375,7 +376,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
     const int unit = blockIdx.x / (SPLIT ? shares : CG), units = gridDim.x / (SPLIT ? shares : CG);
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (warp == 2 && lane < MAX_IN) asm volatile("prefetch.tensormap [%0];" ::"l"(&p.in[lane]) : "memory");      // (of the launch's parameters)
+    if (warp == 2 && (p.in_used >> lane & 1)) asm volatile("prefetch.tensormap [%0];" ::"l"(&p.in[lane]) : "memory");      // (of the launch's parameters)
     if (tid == 0) {
         for (int i = 0; i < NSTAGE; ++i) {
             mbar_init(bar(BAR_FULL + i), 1);
@@ -932,7 +933,11 @@ inline bool make_map_f32(CUtensorMap* tm, const void* base, int slices, long lon
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // operand in 64 x 64 tiles; result in 32-row slabs of 64 columns.  (A row is 2 C bytes: C a multiple of 8.)
-inline bool in_map(CUtensorMap* tm, const void* base, long long rows, long long C) { return make_map(tm, base, rows, C, 64); }
+inline bool in_map(GemmParams& p, int i, const void* base, long long rows, long long C)
+{
+    p.in_used |= 1u << i;
+    return make_map(&p.in[i], base, rows, C, 64);
+}
 inline bool out_map(CUtensorMap* tm, const void* base, long long rows, long long C) { return make_map(tm, base, rows, C, 32); }
 
 inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }

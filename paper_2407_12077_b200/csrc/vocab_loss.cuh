@@ -121,7 +121,7 @@ inline gf_status_t vocab_loss(const __nv_bfloat16* x, const __nv_bfloat16* w, co
     const int n_sm = sm_count();
     if (n_sm < 2) return GF_ERR_CUDA;
     GemmParams p = {};
-    if (!in_map(&p.in[0], x, rows, D) || !in_map(&p.in[1], w, V, D)) return GF_ERR_CUDA;
+    if (!in_map(p, 0, x, rows, D) || !in_map(p, 1, w, V, D)) return GF_ERR_CUDA;
     p.targets = targets;
     p.vocab = V;
     p.stats = static_cast<float2*>(ws);
@@ -157,7 +157,7 @@ inline gf_status_t vocab_loss_backward(const __nv_bfloat16* x, const __nv_bfloat
         const __nv_bfloat16* wp = w + (size_t)v0 * D;
         {
             GemmParams p = {};
-            if (!in_map(&p.in[0], x, rows, D) || !in_map(&p.in[1], wp, cols, D) || !out_map(&p.out[0], P, rows, pitch)) return GF_ERR_CUDA;
+            if (!in_map(p, 0, x, rows, D) || !in_map(p, 1, wp, cols, D) || !out_map(&p.out[0], P, rows, pitch)) return GF_ERR_CUDA;
             p.targets = targets;
             p.vocab = V;
             p.first_col = (int)v0;
@@ -173,7 +173,7 @@ inline gf_status_t vocab_loss_backward(const __nv_bfloat16* x, const __nv_bfloat
         }
         GemmParams p = {};
         const bool first = v0 == 0, last = v0 + step >= V;
-        if (!in_map(&p.in[0], P, rows, pitch) || !in_map(&p.in[1], wp, cols, D) || !in_map(&p.in[2], x, rows, D)) return GF_ERR_CUDA;
+        if (!in_map(p, 0, P, rows, pitch) || !in_map(p, 1, wp, cols, D) || !in_map(p, 2, x, rows, D)) return GF_ERR_CUDA;
         Product q[2];
         gradient_products(q, rows, D, cols, dx, dw + (size_t)v0 * D);
         const gf_status_t s = run_products(p, q, 2, plan, first ? (last ? PART_ONLY : PART_FIRST) : last ? PART_LAST : PART_MIDDLE,

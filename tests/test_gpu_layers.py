@@ -504,6 +504,41 @@ def test_calls_on_another_stream_and_two_at_a_time():
             assert torch.equal(g[k], w[k]), k
 
 
+def test_offsets_past_32_bits():
+    """Tensors of more than 2^32 bytes and 2^31 elements: rows at both ends against the same rows by themselves."""
+    rows, D, V = 1_100_000, 2048, 300
+    ends = torch.cat([torch.arange(128), torch.arange(rows - 128, rows)]).to(DEV)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    block = torch.randn(1000, D, generator=g, device=DEV).to(BF)
+    y = block.repeat(rows // 1000, 1)
+    dout = y.flip(1)
+    dy = gf.layernorm_heads_backward(y.view(rows, 32, 64), dout.view(rows, 32, 64), want_params=False)[0].view(rows, D)
+    few = gf.layernorm_heads_backward(y[ends].view(-1, 32, 64), dout[ends].view(-1, 32, 64), want_params=False)[0].view(-1, D)
+    assert torch.equal(dy[ends], few) and torch.equal(dy[-1000:], dy[:1000])
+    del dy, dout
+    w, x = torch.randn(64, D, generator=g, device=DEV).to(BF) / 8, y[:, :64].contiguous()
+    out = gf.gated_linear(x, w, act="sigmoid")
+    want = gf.gated_linear(x[ends].contiguous(), w, act="sigmoid")
+    assert_near(out[ends], want)
+    dx = gf.gated_linear_backward(x, w, y, act="sigmoid")[0]
+    assert_near(dx[ends], gf.gated_linear_backward(x[ends].contiguous(), w, y[ends], act="sigmoid")[0])
+    del out, y
+    t = torch.randint(0, V, (rows,), generator=g, device=DEV)
+    head = torch.randn(V, 64, generator=g, device=DEV).to(BF)
+    loss, lse = gf.vocab_loss(x, head, t)
+    few = gf.vocab_loss(x[ends].contiguous(), head, t[ends])
+    assert (loss[ends] - few[0]).abs().max() < 1e-4
+    dx = gf.vocab_loss_backward(x, head, t, lse)[0]
+    assert_near(dx[ends], gf.vocab_loss_backward(x[ends].contiguous(), head, t[ends], few[1])[0])
+    gf.last_device_status()
+
+
+def assert_near(a, b):
+    """The same rows through tiles of another shape: an operand and the result rounded to bf16 once each, from sums in another order."""
+    a, b = a.double(), b.double()
+    assert (a - b).norm() <= 2 * HALF * b.norm() and torch.isfinite(a).all()
+
+
 def test_binding_checks_shapes_and_types():
     x, w, x2, w2, dy = dev(*make_gate(16, 64, 72, 136, seed=1))
     for bad in (lambda: gf.gated_linear(x, w, x, w2), lambda: gf.gated_linear(x.float(), w), lambda: gf.gated_linear(x.t().contiguous().t(), w),
