@@ -486,7 +486,8 @@ GF_API gf_status_t gf_gated_linear(const void *x, const void *w, const void *x2,
  *   workspace     DEVICE, gf_gated_linear_backward_workspace_bytes(rows,K1,K2,F,same) bytes, 16-byte aligned, with K2 = 0 without w2 and
  *                 same = 1 where x2 is NULL for x (da and db, and fp32 sums of products that are cut along their
  *                 contraction index, on the current device); GF_ERR_WORKSPACE if absent or too small
- * relu^2 has derivative 0 at 0.  da and db are rounded to bf16 (they are operands of the second products), sums are fp32, results
+ * relu^2 has derivative 0 at 0.  da and db are rounded to bf16 (they are operands of the second products; of up to 128 rows what the
+ * rounding leaves is multiplied as well), sums are fp32, results
  * rounded once, in an order that the sizes and the GPU alone decide.  rows = 0 writes zeros to dw and dw2.  Enqueues two kernels on
  * `stream` (three where a product is cut), allocates nothing, does not synchronise. */
 GF_API gf_status_t gf_gated_linear_backward(const void *x, const void *w, const void *x2, const void *w2, int act,
@@ -514,9 +515,9 @@ GF_API size_t gf_vocab_loss_workspace_bytes(long long rows, long long V);
  *   x, w, targets, sizes   as for gf_vocab_loss, lse what it wrote;   dloss  DEVICE fp32 [rows] (alignment as lse), or NULL for 1 in every row
  *   dx [rows][D], dw [V][D]   DEVICE bf16, written; neither may be an input
  *   workspace  DEVICE, gf_vocab_loss_backward_workspace_bytes(rows,D,V) bytes, 16-byte aligned; GF_ERR_WORKSPACE if absent or
- *              too small (256 MB for a piece of P, 2 KB per row at least; fp32 sums of dx where the vocabulary takes several pieces, and of
+ *              too small (256 MB for a piece of P, 2 KB per row at least, twice that for up to 128 rows; fp32 sums of dx where the vocabulary takes several pieces, and of
  *              products that are cut along their contraction index, 256 MB at most)
- * P is rounded to bf16 (it is an operand of both products), sums are fp32, results rounded once, in an order that the sizes and the GPU
+ * P is rounded to bf16 (it is an operand of both products; of up to 128 rows what the rounding leaves is multiplied as well), sums are fp32, results rounded once, in an order that the sizes and the GPU
  * alone decide.  rows = 0 writes zeros to dw.  Enqueues two kernels per piece of the vocabulary on `stream` (three where a product is
  * cut), allocates nothing, does not synchronise. */
 GF_API gf_status_t gf_vocab_loss_backward(const void *x, const void *w, const int64_t *targets, const float *lse,

@@ -69,9 +69,8 @@ inline Launch forward_launch(const Shape& s, int n_sm, bool clusters, bool split
         time = rounds(m2 * ceil_div(s.F, 2 * w), n_sm / 2) * s1 * STEP_TIME[2];
         offer(1, TILES, 1, rounds(m1 * ceil_div(s.F, w), n_sm) * s1 * STEP_TIME[1]);
     } else {
-        time = rounds(m2 * ceil_div(s.F, 256), n_sm / 2) * (both + 2) * STEP_TIME[2];
-        best.mode = WIDE_TILES;
-        offer(2, TILES, 2, rounds(m2 * ceil_div(s.F, 128), n_sm / 2) * both * 5);
+        time = rounds(m2 * ceil_div(s.F, 128), n_sm / 2) * both * 5;
+        offer(2, WIDE_TILES, 2, rounds(m2 * ceil_div(s.F, 256), n_sm / 2) * (both + 2) * STEP_TIME[2]);
         offer(1, TILES, 1, rounds(m1 * ceil_div(s.F, 64), n_sm) * both * 6);
     }
     const long long tiles = m1 * ceil_div(s.F, 128);
@@ -100,23 +99,36 @@ inline gf_status_t gated_linear(const __nv_bfloat16* x, const __nv_bfloat16* w, 
 }
 
 namespace gl {
-// The gradient's products.  Maps 0: da, 1: db, 2: w, 3: w2, 4: x, 5: x2.
+// The gradient's products.  Maps 0: da, 1: db, 2: w, 3: w2, 4: x, 5: x2, 6, 7: what rounding left of da, db (keep_rests()).
 inline int gradient_products(const Shape& s, Product (&q)[MAX_GROUPS], __nv_bfloat16* dx, __nv_bfloat16* dw, __nv_bfloat16* dx2, __nv_bfloat16* dw2)
 {
+    const bool gated = s.K2 > 0, rests = keep_rests(s.rows);
     int n = 0;
-    q[n++] = Product{s.rows, s.K1, 1, {segment(0, false, 2, false, s.F)}, dx};
-    if (s.K2 > 0 && s.same) q[0].seg[q[0].n_seg++] = segment(1, false, 3, false, s.F);
-    q[n++] = Product{s.K1, s.F, 1, {segment(4, true, 0, true, s.rows)}, dw};
-    if (s.K2 > 0) {
-        q[n++] = Product{s.K2, s.F, 1, {segment(5, true, 1, true, s.rows)}, dw2};
-        if (!s.same) q[n++] = Product{s.rows, s.K2, 1, {segment(1, false, 3, false, s.F)}, dx2};
+    auto add = [](Product& p, const Segment& g) { p.seg[p.n_seg++] = g; };
+    auto by_weights = [&](Product& p, int d, int w) {            // d w^T
+        add(p, segment(d, false, w, false, s.F));
+        if (rests) add(p, segment(d + 6, false, w, false, s.F));
+    };
+    auto by_inputs = [&](Product& p, int x, int d) {             // x^T d
+        add(p, segment(x, true, d, true, s.rows));
+        if (rests) add(p, segment(x, true, d + 6, true, s.rows));
+    };
+    Product& px = q[n++] = Product{s.rows, s.K1, 0, {}, dx};
+    by_weights(px, 0, 2);
+    if (gated && s.same) by_weights(px, 1, 3);
+    by_inputs(q[n++] = Product{s.K1, s.F, 0, {}, dw}, 4, 0);
+    if (gated) {
+        by_inputs(q[n++] = Product{s.K2, s.F, 0, {}, dw2}, 5, 1);
+        if (!s.same) by_weights(q[n++] = Product{s.rows, s.K2, 0, {}, dx2}, 1, 3);
     }
     return n;
 }
-inline size_t operand_bytes(const Shape& s) { return ((size_t)s.rows * s.F * 2 * (s.K2 > 0 ? 2 : 1) + 255) & ~(size_t)255; }
+inline size_t one_operand(const Shape& s) { return ((size_t)s.rows * s.F * 2 + 255) & ~(size_t)255; }
+inline size_t operand_bytes(const Shape& s) { return one_operand(s) * (s.K2 > 0 ? 2 : 1) * (keep_rests(s.rows) ? 2 : 1); }
 }  // namespace gl
 
-// Workspace of the gradient: da and, where there is a second product, db, [rows][F] bf16 each, and the sums of products that are cut.
+// Workspace of the gradient: da and, where there is a second product, db, [rows][F] bf16 each (and of few rows what rounding left of them), and the sums of
+// products that are cut.
 inline size_t gated_linear_backward_bytes(const gl::Shape& s)
 {
     pg::Product q[pg::MAX_GROUPS];
@@ -131,21 +143,25 @@ inline gf_status_t gated_linear_backward(const __nv_bfloat16* x, const __nv_bflo
     using namespace gl;
     const int n_sm = sm_count();
     if (n_sm < 2) return GF_ERR_CUDA;
-    const bool gated = s.K2 > 0;
-    __nv_bfloat16 *da = ws, *db = ws + (size_t)s.rows * s.F;
+    const bool gated = s.K2 > 0, rests = keep_rests(s.rows);
+    __nv_bfloat16* d[4];                              // da, db, and what rounding left of them
+    for (int i = 0; i < 4; ++i) d[i] = ws + one_operand(s) / 2 * (gated ? i : i / 2);
     bool done = false;
     for (const bool clusters : {true, false}) {
         GemmParams p = {};
         p.act = act;
         p.dy = dy;
-        const Launch l = forward_launch(s, n_sm, clusters, false);
-        if (!products(p, l, s, x, w, x2, w2) || !out_map(&p.out[0], da, s.rows, s.F) || (gated && !out_map(&p.out[1], db, s.rows, s.F))) return GF_ERR_CUDA;
-        if ((done = launch<EPI_GATE_GRAD>(l, p, st, launches))) break;
+        const Launch l = rests ? SINGLE : forward_launch(s, n_sm, clusters, false);
+        if (!products(p, l, s, x, w, x2, w2)) return GF_ERR_CUDA;
+        for (int i = 0; i < 4; ++i)
+            if ((i % 2 == 0 || gated) && (i < 2 || rests) && !out_map(&p.out[i], d[i], s.rows, s.F)) return GF_ERR_CUDA;
+        if ((done = rests ? launch<EPI_GATE_GRAD_RESTS>(l, p, st, launches) : launch<EPI_GATE_GRAD>(l, p, st, launches))) break;
     }
     if (!done) return GF_ERR_CUDA;
     GemmParams p = {};
-    if (!in_map(p, 0, da, s.rows, s.F) || !in_map(p, 2, w, s.K1, s.F) || !in_map(p, 4, x, s.rows, s.K1)) return GF_ERR_CUDA;
-    if (gated && (!in_map(p, 1, db, s.rows, s.F) || !in_map(p, 3, w2, s.K2, s.F) || !in_map(p, 5, x2, s.rows, s.K2))) return GF_ERR_CUDA;
+    if (!in_map(p, 0, d[0], s.rows, s.F) || !in_map(p, 2, w, s.K1, s.F) || !in_map(p, 4, x, s.rows, s.K1) || (rests && !in_map(p, 6, d[2], s.rows, s.F))) return GF_ERR_CUDA;
+    if (gated && (!in_map(p, 1, d[1], s.rows, s.F) || !in_map(p, 3, w2, s.K2, s.F) || !in_map(p, 5, x2, s.rows, s.K2) || (rests && !in_map(p, 7, d[3], s.rows, s.F))))
+        return GF_ERR_CUDA;
     Product q[MAX_GROUPS];
     const int n = gradient_products(s, q, dx, dw, dx2, dw2);
     Plan plan = plan_products(q, n, plan_sms(), false);

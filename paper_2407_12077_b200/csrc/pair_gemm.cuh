@@ -55,13 +55,20 @@ enum Epilogue {
     EPI_GATE,           // act(a) * b of the two halves, or act(a) of a whole tile
     EPI_GATE_GRAD,      // dy b act'(a) and dy act(a)
     EPI_LSE,            // per row and tile of columns: maximum and sum of exponentials, and the target's logit
-    EPI_PROB            // (exp(z - lse) - [column is the target]) * dloss
+    EPI_PROB,           // (exp(z - lse) - [column is the target]) * dloss
+    // the same two, and what rounding an output to bf16 leaves of it in a tensor of its own (maps out[2], out[3]; out[1])
+    EPI_GATE_GRAD_RESTS,
+    EPI_PROB_RESTS
 };
+constexpr bool is_gate_grad(Epilogue e) { return e == EPI_GATE_GRAD || e == EPI_GATE_GRAD_RESTS; }
+constexpr bool is_prob(Epilogue e) { return e == EPI_PROB || e == EPI_PROB_RESTS; }
+constexpr bool has_rests(Epilogue e) { return e == EPI_GATE_GRAD_RESTS || e == EPI_PROB_RESTS; }
 enum Mode { TILES, WIDE_TILES, SPLIT_TILES };
 enum BCols : unsigned char { B_WHOLE, B_DUAL, B_HALF };
 enum OutMode : unsigned char { OUT_BF16, OUT_F32, OUT_F32_ADD, OUT_BF16_ADD };   // (_ADD: onto, resp. with, the fp32 sums of earlier launches; F32: [slices][rows][cols])
 enum Act { ACT_SIGMOID = 0, ACT_RELU2 = 1, ACT_SILU = 2, ACT_GELU = 3 };
 
+constexpr int MAX_IN = 8, MAX_OUT = 4, MAX_GROUPS = 4, MAX_SEGMENTS = 4;
 // A run of contraction indices of a group's products: 64 * steps of them (the last may reach past the tensors, where TMA reads zeros).
 struct Segment {
     unsigned char a, b;             // tensor maps (B_DUAL: b and b + 1)
@@ -76,13 +83,12 @@ struct Group {
     int slices;                     // tiles per place of the result, each with its share of the contraction indices (all segments' in a row)
     int steps;                      // of all segments
     int n_seg;
-    Segment seg[2];
+    Segment seg[MAX_SEGMENTS];
     unsigned char out;              // tensor map of the result
     OutMode mode;
     int rows, cols;                 // extent of the result (of each half's columns where a tile is halved)
     float* part;                    // OUT_BF16_ADD: fp32 sums [rows][cols]
 };
-constexpr int MAX_IN = 8, MAX_OUT = 4, MAX_GROUPS = 4;
 struct GemmParams {
     CUtensorMap in[MAX_IN], out[MAX_OUT];
     Group g[MAX_GROUPS];
@@ -284,6 +290,15 @@ __device__ __forceinline__ void ld_acc2(uint32_t t0, float (&a)[32], uint32_t t1
         : "r"(t0), "r"(t1) : "memory");
 }
 
+// v <- v minus its rounding to bf16 (nothing of an infinity or a NaN: the rounded value carries it)
+__device__ __forceinline__ void leave_rest(float (&v)[32])
+{
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        const float r = v[j] - __bfloat162float(__float2bfloat16_rn(v[j]));
+        v[j] = fabsf(r) < INFINITY ? r : 0.f;
+    }
+}
 struct Tile {
     int g, m, n;                    // group, place in it
     int slice, lo, hi;              // the steps it takes
@@ -525,12 +540,12 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
         struct RowValues { long long target; float lse, weight; };
         auto row_values = [&](const Tile& t) {
             RowValues v = {-1, 0.f, 0.f};
-            if constexpr (EPI == EPI_LSE || EPI == EPI_PROB) {
+            if constexpr (EPI == EPI_LSE || is_prob(EPI)) {
                 const int r = t.m * 128 * CG + 128 * (int)rank + 32 * sp + lane;
                 if (r < p.g[t.g].rows) {
                     v.target = p.targets[r];
                     if (v.target < 0 || v.target >= p.vocab) v.target = -1;
-                    if constexpr (EPI == EPI_PROB) {
+                    if constexpr (is_prob(EPI)) {
                         v.lse = p.lse[r];
                         v.weight = v.target < 0 ? 0.f : p.dloss ? p.dloss[r] : 1.f;
                     }
@@ -548,10 +563,10 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
             const int row0 = tm * 128 * CG + 128 * (int)rank + 32 * sp, row = row0 + lane;
             const bool in = row < g.rows;
             // what the epilogue reads from memory is under way while the products run
-            const int width = EPI == EPI_GATE || EPI == EPI_GATE_GRAD ? (WIDE || p.gated ? HW : BN) : BN;
+            const int width = EPI == EPI_GATE || is_gate_grad(EPI) ? (WIDE || p.gated ? HW : BN) : BN;
             uint32_t dy[2][16];                       // of the warp's first block of 64 columns
             auto load_dy = [&](int c) {
-                if constexpr (EPI == EPI_GATE_GRAD) {
+                if constexpr (is_gate_grad(EPI)) {
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const int col = tn * width + c + 32 * half;
@@ -737,11 +752,12 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                     }
                     send(&p.out[0], col);
                 }
-            } else if constexpr (EPI == EPI_GATE_GRAD) {
+            } else if constexpr (is_gate_grad(EPI)) {
+                for (int rest = 0; rest <= (int)has_rests(EPI); ++rest)
                 for (int c = 64 * part; c < width; c += 128) {
                     const int col = tn * width + c;
                     if (col >= g.cols) break;
-                    if (c >= 128) load_dy(c);
+                    if (c >= 128 || rest) load_dy(c);
                     take_slab();
                     uint32_t later[2][16];            // db, in bf16, until da has left the slab
 #pragma unroll
@@ -760,6 +776,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                                     b[j] = bf16_at(d, j) * f;
                                 }
                             });
+                            if (rest) leave_rest(b);
 #pragma unroll
                             for (int j = 0; j < 16; ++j) later[half][j] = pack_bf16(b[2 * j], b[2 * j + 1]);
                         } else {
@@ -773,15 +790,16 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                                 }
                             });
                         }
+                        if (rest) leave_rest(a);
                         put_bf16(sl, lane, half, a);
                     }
-                    send(&p.out[0], col);
+                    send(&p.out[2 * rest], col);
                     if (p.gated) {
                         take_slab();
 #pragma unroll
                         for (int q = 0; q < 8; ++q)
                             sts128(sl + swz(lane, q << 4), later[q / 4][4 * (q % 4)], later[q / 4][4 * (q % 4) + 1], later[q / 4][4 * (q % 4) + 2], later[q / 4][4 * (q % 4) + 3]);
-                        send(&p.out[1], col);
+                        send(&p.out[2 * rest + 1], col);
                     }
                 }
             } else if constexpr (EPI == EPI_LSE) {
@@ -828,6 +846,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                 if (in) p.stats[(size_t)(2 * tn + part) * g.rows + row] = make_float2(ref, sum);
             } else {
                 const long long at = target < 0 ? -1 : target - p.first_col;
+                for (int rest = 0; rest <= (int)has_rests(EPI); ++rest)
                 for (int c = 64 * part; c < BN; c += 128) {
                     const int col = tn * BN + c;
                     if (col >= g.cols) break;
@@ -858,9 +877,10 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                             for (int j = 0; j < 32; ++j)
                                 if (col + 32 * half + j >= g.cols) v[j] = 0.f;
                         }
+                        if (rest) leave_rest(v);
                         put_bf16(sl, lane, half, v);
                     }
-                    send(&p.out[g.out], col);
+                    send(&p.out[rest], col);
                 }
             }
             tc_fence_before();
@@ -1014,7 +1034,9 @@ inline bool launch(const Launch& l, const GemmParams& p, cudaStream_t st, std::a
     const int n_sm = sm_count(), dev = current_device();
     if (n_sm < 2 || dev < 0) return false;
     cudaError_t e = cudaErrorInvalidValue;
-    if (l.mode == TILES) e = l.cg == 2 ? launch_one<2, EPI, TILES>(p, n_sm, dev, st) : launch_one<1, EPI, TILES>(p, n_sm, dev, st);
+    if (l.mode == TILES && l.cg == 1) e = launch_one<1, EPI, TILES>(p, n_sm, dev, st);
+    if constexpr (!has_rests(EPI))                    // (few rows: SINGLE)
+        if (l.mode == TILES && l.cg == 2) e = launch_one<2, EPI, TILES>(p, n_sm, dev, st);
     if constexpr (EPI == EPI_GATE || EPI == EPI_GATE_GRAD)
         if (l.mode == WIDE_TILES) e = launch_one<2, EPI, WIDE_TILES>(p, n_sm, dev, st);
     if constexpr (EPI == EPI_GATE)
@@ -1028,6 +1050,12 @@ inline bool launch(const Launch& l, const GemmParams& p, cudaStream_t st, std::a
 }
 
 // ---------------------------------------------------------------- several products in one launch (a gradient's)
+// A gradient's first operand (da, db, P) is rounded to bf16.  Over many rows the roundings average out to about the result's own (2.3e-3 of the
+// result's norm in all, the result's rounding alone being 1.7e-3); with few rows a few large values carry the result, and the error with
+// them (up to 2.7e-3).  There what the rounding leaves is kept too, in a second bf16 tensor, and multiplied as well: such calls wait for
+// launches and weights, not for products (24 rows, 424 deep -> 2072, gated: 17 us -> 25; 20 rows, 1704 deep, over 14752 entries: 64 -> 76).
+constexpr long long REST_ROWS = 128;
+inline bool keep_rests(long long rows) { return rows <= REST_ROWS; }
 // Time of 64 contraction indices, in units of 1/30 us.  An SM takes in 64 bytes per cycle: the 32 KB of its share of a pair's 256 x 256 products
 // take as long as these do, and the 32 KB of a 128 x 128 tile of its own hardly less (8192 deep, one tile: 0.264 us a step), for a
 // half of the work per SM.
@@ -1036,9 +1064,14 @@ constexpr int STEP_TIME[3] = {0, 7, 8};
 struct Product {
     long long m, n;
     int n_seg;
-    Segment seg[2];
+    Segment seg[MAX_SEGMENTS];
     __nv_bfloat16* out;             // [m][n]
-    int steps() const { return seg[0].steps + (n_seg > 1 ? seg[1].steps : 0); }
+    int steps() const
+    {
+        int n = 0;
+        for (int i = 0; i < n_seg; ++i) n += seg[i].steps;
+        return n;
+    }
 };
 // Of a sum that several launches contribute to (pieces of the vocabulary)
 enum Part { PART_ONLY, PART_FIRST, PART_MIDDLE, PART_LAST };

@@ -94,11 +94,12 @@ inline size_t round_256(size_t n) { return (n + 255) & ~(size_t)255; }
 inline size_t vocab_stats_bytes(long long rows, long long V) { return round_256((size_t)rows * 2 * pg::ceil_div(V, 128) * sizeof(float2)); }
 inline size_t vocab_loss_bytes(long long rows, long long V) { return vocab_stats_bytes(rows, V) + (size_t)rows * 4; }
 namespace vl {
-// A piece's products: its part of dx (map 0: P, 1: the piece's rows of W) and its rows of dW (2: x).
+// A piece's products: its part of dx (map 0: P, 1: the piece's rows of W) and its rows of dW (2: x); 3: what rounding left of P (keep_rests()).
 inline void gradient_products(Product (&q)[2], long long rows, int D, long long cols, __nv_bfloat16* dx, __nv_bfloat16* dw)
 {
-    q[0] = Product{rows, D, 1, {segment(0, false, 1, true, cols)}, dx};
-    q[1] = Product{cols, D, 1, {segment(0, true, 2, true, rows)}, dw};
+    const int n = keep_rests(rows) ? 2 : 1;
+    q[0] = Product{rows, D, n, {segment(0, false, 1, true, cols), segment(3, false, 1, true, cols)}, dx};
+    q[1] = Product{cols, D, n, {segment(0, true, 2, true, rows), segment(3, true, 2, true, rows)}, dw};
 }
 // (all pieces are cut like the first, the largest)
 inline Plan gradient_plan(long long rows, int D, long long V)
@@ -108,10 +109,11 @@ inline Plan gradient_plan(long long rows, int D, long long V)
     gradient_products(q, rows, D, step < V ? step : V, nullptr, nullptr);
     return plan_products(q, 2, plan_sms(), step < V);
 }
-inline size_t piece_bytes(long long rows, long long V) { return ((size_t)rows * piece_cols(rows, V) * 2 + 255) & ~(size_t)255; }
+inline size_t one_piece(long long rows, long long V) { return ((size_t)rows * piece_cols(rows, V) * 2 + 255) & ~(size_t)255; }
+inline size_t piece_bytes(long long rows, long long V) { return one_piece(rows, V) * (keep_rests(rows) ? 2 : 1); }
 }  // namespace vl
 
-// Gradient: a piece of P, and fp32 sums of dx over the pieces and of products that are cut.
+// Gradient: a piece of P (of few rows what rounding left of it too), and fp32 sums of dx over the pieces and of products that are cut.
 inline size_t vocab_loss_backward_bytes(long long rows, int D, long long V) { return vl::piece_bytes(rows, V) + vl::gradient_plan(rows, D, V).bytes; }
 
 inline gf_status_t vocab_loss(const __nv_bfloat16* x, const __nv_bfloat16* w, const long long* targets, float* loss, float* lse, long long rows,
@@ -150,22 +152,24 @@ inline gf_status_t vocab_loss_backward(const __nv_bfloat16* x, const __nv_bfloat
     if (n_sm < 2) return GF_ERR_CUDA;
     const long long step = piece_cols(rows, V);
     Plan plan = gradient_plan(rows, D, V);
-    __nv_bfloat16* P = static_cast<__nv_bfloat16*>(ws);
+    __nv_bfloat16 *P = static_cast<__nv_bfloat16*>(ws), *P_rest = P + one_piece(rows, V) / 2;
+    const bool rests = keep_rests(rows);
     for (long long v0 = 0; v0 < V; v0 += step) {
         const long long cols = V - v0 < step ? V - v0 : step;
         const long long pitch = (cols + 7) / 8 * 8;               // (a row of a tensor map is a multiple of 16 bytes; the last columns are zero)
         const __nv_bfloat16* wp = w + (size_t)v0 * D;
         {
             GemmParams p = {};
-            if (!in_map(p, 0, x, rows, D) || !in_map(p, 1, wp, cols, D) || !out_map(&p.out[0], P, rows, pitch)) return GF_ERR_CUDA;
+            if (!in_map(p, 0, x, rows, D) || !in_map(p, 1, wp, cols, D) || !out_map(&p.out[0], P, rows, pitch) || (rests && !out_map(&p.out[1], P_rest, rows, pitch)))
+                return GF_ERR_CUDA;
             p.targets = targets;
             p.vocab = V;
             p.first_col = (int)v0;
             p.lse = lse;
             p.dloss = dloss;
-            const int cg = forward_cg(rows, cols, n_sm);
+            const int cg = rests ? 1 : forward_cg(rows, cols, n_sm);
             logits(p, cg, rows, D, cols);
-            if (!launch<EPI_PROB>(Launch{cg, TILES, cg}, p, st, launches)) {
+            if (!(rests ? launch<EPI_PROB_RESTS>(SINGLE, p, st, launches) : launch<EPI_PROB>(Launch{cg, TILES, cg}, p, st, launches))) {
                 if (cg == 1) return GF_ERR_CUDA;
                 logits(p, 1, rows, D, cols);
                 if (!launch<EPI_PROB>(SINGLE, p, st, launches)) return GF_ERR_CUDA;
@@ -173,7 +177,7 @@ inline gf_status_t vocab_loss_backward(const __nv_bfloat16* x, const __nv_bfloat
         }
         GemmParams p = {};
         const bool first = v0 == 0, last = v0 + step >= V;
-        if (!in_map(p, 0, P, rows, pitch) || !in_map(p, 1, wp, cols, D) || !in_map(p, 2, x, rows, D)) return GF_ERR_CUDA;
+        if (!in_map(p, 0, P, rows, pitch) || !in_map(p, 1, wp, cols, D) || !in_map(p, 2, x, rows, D) || (rests && !in_map(p, 3, P_rest, rows, pitch))) return GF_ERR_CUDA;
         Product q[2];
         gradient_products(q, rows, D, cols, dx, dw + (size_t)v0 * D);
         const gf_status_t s = run_products(p, q, 2, plan, first ? (last ? PART_ONLY : PART_FIRST) : last ? PART_LAST : PART_MIDDLE,

@@ -455,6 +455,37 @@ def test_training_step_through_the_operators_matches_float64_step_by_step():
         assert e <= 9 * HALF, (name, e)
 
 
+@pytest.mark.parametrize("rows", [1, 5, 128])
+def test_gradients_of_few_rows_are_off_by_their_own_rounding_alone(rows):
+    """Of up to 128 rows da, db and P are kept to 16 bits of mantissa (a rounding and what it leaves, each off by HALF of itself), so every element
+    of a gradient is off by its rounding, HALF, and HALF^2 of the magnitudes it is the sum of."""
+    x, w, x2, w2, dy = make_gate(rows, 136, 72, 264, seed=rows)
+    got = gf.gated_linear_backward(*dev(x, w, dy, x2, w2), act="silu")
+    want = orc.gated_linear_backward(x, w, dy, x2, w2, act="silu")
+    a, ea, b, eb, f, ef, df, edf = gate_parts(x, w, x2, w2, "silu")
+    d = np.abs(np64(dy))
+    da, db = d * np.abs(b) * np.abs(df), d * np.abs(f)
+    eda, edb = HALF ** 2 * da + d * (edf * (np.abs(b) + eb) + np.abs(df) * eb), HALF ** 2 * db + d * ef
+    X, W, X2, W2 = (np.abs(np64(t)) for t in (x, w, x2, w2))
+    n = 2 * acc(264)
+    bounds = [eda @ W.T + n * (da @ W.T), X.T @ eda + n * (X.T @ da), edb @ W2.T + n * (db @ W2.T), X2.T @ edb + n * (X2.T @ db)]
+    for name, g, t, e in zip(("dx", "dw", "dx2", "dw2"), got, want, bounds):
+        near(g, t, HALF * np.abs(t) + (1 + HALF) * e + 2.0 ** -126, name)
+    x, w, t, dl = make_loss(rows, 136, 1003, seed=rows)
+    xd, wd, td, dd = dev(x, w, t, dl)
+    lse = gf.vocab_loss(xd, wd, td)[1]
+    got = gf.vocab_loss_backward(xd, wd, td, lse, dd)
+    gf.last_device_status()
+    dx, dw, P = orc.vocab_loss_backward(x, w, t, dl)
+    e = 2 * logit_error(x, w) + 2.0 ** -19 + (64 + 1003 / 128) * 2.0 ** -23 + 2.0 ** -22 * np.abs(np64(lse))
+    has = ((t >= 0) & (t < 1003)).numpy()
+    p = np.abs(P) + np.where(has, np.abs(np64(dl)), 0)[:, None] * (np.arange(1003)[None, :] == t.numpy()[:, None])
+    eP, X, W = (HALF ** 2 + e[:, None]) * p, np.abs(np64(x)), np.abs(np64(w))
+    n = 2 * acc(2 * 1003)
+    near(got[0], dx, HALF * np.abs(dx) + (1 + HALF) * (eP @ W + n * (np.abs(P) @ W)) + 2.0 ** -126, "dx")
+    near(got[1], dw, HALF * np.abs(dw) + (1 + HALF) * (eP.T @ X + n * (np.abs(P).T @ X)) + 2.0 ** -126, "dw")
+
+
 def test_training_step_back_to_back_equals_one_call_at_a_time():
     b = Block(T=1111, H=12, V=4001)
     one = b.step(torch.cuda.synchronize)
