@@ -594,7 +594,7 @@ def fold_summaries(state_in, summaries, n_fold, state_out=None, stream=None):
 
 def layernorm_heads(y, gamma=None, beta=None, eps=1e-5, out=None, stream=None):
     """gf_c2_layernorm(_f32): LayerNorm over all H*N channels of every token.  y: [..., H, N] CUDA tensor
-    (bf16 or fp32, contiguous); gamma, beta: fp32 [H*N] (or [H, N]) or None.  out defaults to a new tensor
+    (bf16 or fp32, contiguous); gamma, beta: fp32 [H*N] (or [H, N], any strides) or None.  out defaults to a new tensor
     (pass out=y for in place).  Returns out."""
     lib = _lib or load_library()
     if _native is not None and stream is None and out is None:
@@ -612,9 +612,9 @@ def layernorm_heads(y, gamma=None, beta=None, eps=1e-5, out=None, stream=None):
     else:
         out_ptr = _dev(out, "out", y.dtype, y.shape)
     with _on(y):
+        gamma, beta = (None if t is None else t.reshape(H * N).contiguous() for t in (gamma, beta))       # (copies, where they are, live until the call)
         _check(getattr(lib, "gf_c2_layernorm" + sfx)(
-            _dev(y, "y"), _dev(None if gamma is None else gamma.reshape(H * N), "gamma", torch.float32),
-            _dev(None if beta is None else beta.reshape(H * N), "beta", torch.float32), float(eps),
+            _dev(y, "y"), _dev(gamma, "gamma", torch.float32), _dev(beta, "beta", torch.float32), float(eps),
             out_ptr, rows, H, N, _stream(stream)), "gf_c2_layernorm" + sfx)
     return out
 
@@ -655,7 +655,7 @@ def _one_device(**tensors) -> None:
 
 def layernorm_heads_backward(y, dout, gamma=None, eps=1e-5, want_params=True, dy=None, stream=None, workspace=None):
     """gf_c2_layernorm_backward(_f32): gradient of layernorm_heads().  y (the forward call's input), dout: [..., H, N] CUDA
-    tensors of one dtype (bf16 or fp32, contiguous); gamma: fp32 [H*N] (or [H, N]) or None.  Returns (dy, dgamma, dbeta), the
+    tensors of one dtype (bf16 or fp32, contiguous); gamma: fp32 [H*N] (or [H, N], any strides) or None.  Returns (dy, dgamma, dbeta), the
     latter two fp32 [H*N] (None unless want_params).  dy defaults to a new tensor (y or dout: in place); the workspace, unless a
     uint8 tensor of enough bytes is passed, is allocated here."""
     lib = _lib or load_library()
@@ -671,7 +671,7 @@ def layernorm_heads_backward(y, dout, gamma=None, eps=1e-5, want_params=True, dy
     dt, f32 = y.dtype, torch.float32
     sfx = _suffix(dt)
     _one_device(y=y, dout=dout, gamma=gamma, dy=dy, workspace=workspace)
-    gamma = None if gamma is None else gamma.reshape(D)       # (a copy, where it is one, lives until the call)
+    gamma = None if gamma is None else gamma.reshape(D).contiguous()       # (a copy, where it is one, lives until the call)
     ins = [_dev(y, "y"), _dev(gamma, "gamma", f32), float(eps), _dev(dout, "dout", dt, y.shape)]
     if dy is None:
         dy = torch.empty_like(y)
