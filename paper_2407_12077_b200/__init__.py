@@ -4,6 +4,9 @@ Every function mirrors the entry point of the same name in ``include/gf_wkv6.h``
 torch tensors supply device memory and the current CUDA stream, all arithmetic runs
 in the library's kernels.  There is no CPU or PyTorch fallback: if the shared library
 is missing or a tensor is not on a CUDA device the call raises.
+
+stream=: a torch.cuda.Stream or a raw handle, for a launch on another stream than the current one.  The call neither waits for the current stream nor
+makes it wait; the tensors that it allocates and returns are that stream's, as under torch.cuda.stream().
 """
 from __future__ import annotations
 
@@ -187,11 +190,21 @@ class _Here:
 _HERE = _Here()
 
 
-def _on(t: torch.Tensor):
-    """Context in which the tensor's device is the current one.  torch.cuda.device costs microseconds of host time per
-    call (the pass of one short prompt: 21.9 us with it, 15.3 us without), so it is only entered when the
-    device has to change."""
-    return _HERE if t.get_device() == torch.cuda.current_device() else torch.cuda.device(t.device)
+def _on(t: torch.Tensor, stream=None, makes=True):
+    """Context in which the tensor's device is the current one and, for a call that makes tensors (outputs, a workspace, a copy of an argument),
+    `stream`, where one is passed, the current stream: the caching allocator then hands none of that memory on before the call's
+    kernels have run.  (Memory made on another stream is free for that stream's next tensor as soon as the call has returned.)
+    torch.cuda.device costs microseconds of host time per call (the pass of one short prompt: 21.9 us with it, 15.3 us without), as
+    torch.cuda.stream does, so they are only entered when something has to change."""
+    index = t.get_device()
+    if index < 0:                          # (not a CUDA tensor: _dev says so)
+        return _HERE
+    if stream is not None:
+        if isinstance(stream, torch.cuda.Stream) and stream.device_index != index:
+            raise ValueError(f"stream on device {stream.device_index}, tensors on device {index}")
+        if makes and (index != torch.cuda.current_device() or _stream(stream) != torch._C._cuda_getCurrentRawStream(index)):
+            return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream), device=index))
+    return _HERE if index == torch.cuda.current_device() else torch.cuda.device(index)
 
 
 def _dev(t: torch.Tensor | None, name: str, dtype=None, shape=None):
@@ -261,12 +274,14 @@ def _workspace_need(device_index, B, T, H, N) -> int:
     return workspace_bytes(B, T, H, N)
 
 
-def _ensure_workspace(B, T, H, N, device) -> None:
-    """Device memory is torch's job: grow the registered scratch when a call could use more."""
+def _ensure_workspace(B, T, H, N, r, stream) -> None:
+    """Device memory is torch's job: grow the registered scratch when a call (of r, on `stream`) could use more."""
+    device = r.device
     need = _workspace_need(device.index, B, T, H, N)
     have = 0 if _workspace is None or _workspace.device != device else _workspace.numel()
     if need > have:
-        set_workspace(torch.empty(need, dtype=torch.uint8, device=device))
+        with _on(r, stream):
+            set_workspace(torch.empty(need, dtype=torch.uint8, device=device))
 
 
 def last_device_status(stream=None) -> None:
@@ -300,23 +315,23 @@ def prefill(r, k, v, x, u, state_in=None, state_out=None, y=None, stream=None, w
     B, T, H, N = shape
     dt = r.dtype
     sfx = _suffix(dt)
-    if y is None:
-        y = torch.empty_like(r)
-        y_ptr = y.data_ptr()
-    else:
-        y_ptr = _dev(y, "y", dt, shape)
-    if state_out is None and want_state:
-        state_out = _new_states(B, H, N, r.device)
-        s_ptr = state_out.data_ptr()
-    else:
-        s_ptr = _dev(state_out, "state_out", torch.float32, (B, H, N, N))
-    args = [_dev(r, "r", shape=shape), _dev(k, "k", dt, shape), _dev(v, "v", dt, shape),
-            _dev(x, "x", dt, shape), _dev(u, "u", torch.float32, (H, N)),
-            _dev(state_in, "state_in", torch.float32, (B, H, N, N)),
-            s_ptr, y_ptr]
-    with _on(r):
+    with _on(r, stream, y is None or (state_out is None and want_state)):
+        if y is None:
+            y = torch.empty_like(r)
+            y_ptr = y.data_ptr()
+        else:
+            y_ptr = _dev(y, "y", dt, shape)
+        if state_out is None and want_state:
+            state_out = _new_states(B, H, N, r.device)
+            s_ptr = state_out.data_ptr()
+        else:
+            s_ptr = _dev(state_out, "state_out", torch.float32, (B, H, N, N))
+        args = [_dev(r, "r", shape=shape), _dev(k, "k", dt, shape), _dev(v, "v", dt, shape),
+                _dev(x, "x", dt, shape), _dev(u, "u", torch.float32, (H, N)),
+                _dev(state_in, "state_in", torch.float32, (B, H, N, N)),
+                s_ptr, y_ptr]
         if sfx == "" and split:
-            _ensure_workspace(B, T, H, N, r.device)
+            _ensure_workspace(B, T, H, N, r, stream)
         elif not split and _workspace is not None:
             set_workspace(None)
         _check(getattr(lib, "gf_wkv6_prefill" + sfx)(*args, B, T, H, N, _stream(stream)), "gf_wkv6_prefill" + sfx)
@@ -339,10 +354,10 @@ def backward(r, k, v, x, u, dy, state_in=None, dstate_out=None, want_dstate=True
         if dt == f32 or workspace is None:
             raise ValueError("backward(saved=True) needs bf16 tensors and the workspace prefill_train() filled")
         sfx = "_saved"
-    dr, dk, dv, dx = (torch.empty_like(r) for _ in range(4))
-    du = torch.empty((H, N), device=r.device, dtype=f32)
-    ds0 = torch.empty((B, H, N, N), device=r.device, dtype=f32) if want_dstate else None
-    with _on(r):
+    with _on(r, stream):
+        dr, dk, dv, dx = (torch.empty_like(r) for _ in range(4))
+        du = torch.empty((H, N), device=r.device, dtype=f32)
+        ds0 = torch.empty((B, H, N, N), device=r.device, dtype=f32) if want_dstate else None
         nbytes = int(getattr(lib, wsfn)(B, T, H, N))
         ws = workspace if workspace is not None and workspace.numel() >= nbytes else torch.empty(max(nbytes, 16), dtype=torch.uint8, device=r.device)
         args = [_dev(r, "r", dt), _dev(k, "k", dt, r.shape), _dev(v, "v", dt, r.shape), _dev(x, "x", dt, r.shape),
@@ -360,9 +375,9 @@ def backward_c2(r, k, v, x, dy, state_in=None, dstate_out=None, want_dstate=True
     lib = load_library()
     B, T, H, N = r.shape
     bf, f32 = torch.bfloat16, torch.float32
-    dr, dk, dv, dx = (torch.empty_like(r) for _ in range(4))
-    ds0 = torch.empty((B, H, N, N), device=r.device, dtype=f32) if want_dstate else None
-    with _on(r):
+    with _on(r, stream):
+        dr, dk, dv, dx = (torch.empty_like(r) for _ in range(4))
+        ds0 = torch.empty((B, H, N, N), device=r.device, dtype=f32) if want_dstate else None
         nbytes = int(lib.gf_wkv6_backward_bf16_workspace_bytes(B, T, H, N))
         ws = workspace if workspace is not None and workspace.numel() >= nbytes else torch.empty(max(nbytes, 16), dtype=torch.uint8, device=r.device)
         args = [_dev(r, "r", bf), _dev(k, "k", bf, r.shape), _dev(v, "v", bf, r.shape), _dev(x, "x", bf, r.shape),
@@ -386,10 +401,10 @@ def backward_varlen(r, k, v, x, u, dy, cu_seqlens, max_seqlen, state_in=None, ds
     total_T, H, N = r.shape
     S = cu_seqlens.numel() - 1
     bf, f32 = torch.bfloat16, torch.float32
-    dr, dk, dv, dx = (torch.empty_like(r) for _ in range(4))
-    du = None if c2 else torch.empty((H, N), device=r.device, dtype=f32)
-    ds0 = torch.empty((S, H, N, N), device=r.device, dtype=f32) if want_dstate else None
-    with _on(r):
+    with _on(r, stream):
+        dr, dk, dv, dx = (torch.empty_like(r) for _ in range(4))
+        du = None if c2 else torch.empty((H, N), device=r.device, dtype=f32)
+        ds0 = torch.empty((S, H, N, N), device=r.device, dtype=f32) if want_dstate else None
         nbytes = int(lib.gf_wkv6_backward_varlen_workspace_bytes(S, total_T, H, N))
         ws = workspace if workspace is not None and workspace.numel() >= nbytes else torch.empty(max(nbytes, 16), dtype=torch.uint8, device=r.device)
         args = [_dev(r, "r", bf), _dev(k, "k", bf, r.shape), _dev(v, "v", bf, r.shape), _dev(x, "x", bf, r.shape)]
@@ -418,9 +433,9 @@ def prefill_train(r, k, v, x, u, workspace, state_in=None, c2=False, u2=None, st
     shape = r.shape
     B, T, H, N = shape
     bf, f32 = torch.bfloat16, torch.float32
-    y = torch.empty_like(r)
-    s_out = _new_states(B, H, N, r.device)
-    with _on(r):
+    with _on(r, stream):
+        y = torch.empty_like(r)
+        s_out = _new_states(B, H, N, r.device)
         base = [_dev(r, "r", bf), _dev(k, "k", bf, shape), _dev(v, "v", bf, shape), _dev(x, "x", bf, shape)]
         mid = _dev(u2, "u2", bf, shape) if c2 else _dev(u, "u", f32, (H, N))
         fn = "gf_wkv6_prefill_c2_train" if c2 else "gf_wkv6_prefill_train"
@@ -446,9 +461,9 @@ def prefill_varlen_train(r, k, v, x, u, cu_seqlens, max_seqlen, workspace, state
     total_T, H, N = shape
     S = cu_seqlens.numel() - 1
     bf, f32 = torch.bfloat16, torch.float32
-    y = torch.empty_like(r)
-    s_out = _new_states(S, H, N, r.device)
-    with _on(r):
+    with _on(r, stream):
+        y = torch.empty_like(r)
+        s_out = _new_states(S, H, N, r.device)
         base = [_dev(r, "r", bf), _dev(k, "k", bf, shape), _dev(v, "v", bf, shape), _dev(x, "x", bf, shape)]
         mid = _dev(u2, "u2", bf, shape) if c2 else _dev(u, "u", f32, (H, N))
         fn = "gf_wkv6_prefill_varlen_c2_train" if c2 else "gf_wkv6_prefill_varlen_train"
@@ -476,22 +491,22 @@ def prefill_c2(r, k, v, x, u2=None, state_in=None, state_out=None, y=None, strea
     shape = r.shape
     B, T, H, N = shape
     bf = torch.bfloat16
-    if y is None:
-        y = torch.empty_like(r)
-        y_ptr = y.data_ptr()
-    else:
-        y_ptr = _dev(y, "y", bf, shape)
-    if state_out is None and want_state:
-        state_out = _new_states(B, H, N, r.device)
-        s_ptr = state_out.data_ptr()
-    else:
-        s_ptr = _dev(state_out, "state_out", torch.float32, (B, H, N, N))
-    args = [_dev(r, "r", bf), _dev(k, "k", bf, shape), _dev(v, "v", bf, shape), _dev(x, "x", bf, shape),
-            _dev(u2, "u2", bf, shape), _dev(state_in, "state_in", torch.float32, (B, H, N, N)),
-            s_ptr, y_ptr]
-    with _on(r):
+    with _on(r, stream, y is None or (state_out is None and want_state)):
+        if y is None:
+            y = torch.empty_like(r)
+            y_ptr = y.data_ptr()
+        else:
+            y_ptr = _dev(y, "y", bf, shape)
+        if state_out is None and want_state:
+            state_out = _new_states(B, H, N, r.device)
+            s_ptr = state_out.data_ptr()
+        else:
+            s_ptr = _dev(state_out, "state_out", torch.float32, (B, H, N, N))
+        args = [_dev(r, "r", bf), _dev(k, "k", bf, shape), _dev(v, "v", bf, shape), _dev(x, "x", bf, shape),
+                _dev(u2, "u2", bf, shape), _dev(state_in, "state_in", torch.float32, (B, H, N, N)),
+                s_ptr, y_ptr]
         if split:
-            _ensure_workspace(B, T, H, N, r.device)
+            _ensure_workspace(B, T, H, N, r, stream)
         elif _workspace is not None:
             set_workspace(None)
         _check(lib.gf_wkv6_prefill_c2(*args, B, T, H, N, _stream(stream)), "gf_wkv6_prefill_c2")
@@ -512,23 +527,23 @@ def prefill_varlen_c2(r, k, v, x, u2, cu_seqlens, max_seqlen, state_in=None, sta
     total_T, H, N = shape
     S = cu_seqlens.numel() - 1
     bf = torch.bfloat16
-    if y is None:
-        y = torch.empty_like(r)
-        y_ptr = y.data_ptr()
-    else:
-        y_ptr = _dev(y, "y", bf, shape)
-    if state_out is None and want_state:
-        state_out = _new_states(S, H, N, r.device)
-        s_ptr = state_out.data_ptr()
-    else:
-        s_ptr = _dev(state_out, "state_out", torch.float32, (S, H, N, N))
-    args = [_dev(r, "r", bf), _dev(k, "k", bf, shape), _dev(v, "v", bf, shape), _dev(x, "x", bf, shape),
-            _dev(u2, "u2", bf, shape), _dev(state_in, "state_in", torch.float32, (S, H, N, N)),
-            s_ptr, y_ptr,
-            _dev(cu_seqlens, "cu_seqlens", torch.int32)]
-    with _on(r):
+    with _on(r, stream, y is None or (state_out is None and want_state)):
+        if y is None:
+            y = torch.empty_like(r)
+            y_ptr = y.data_ptr()
+        else:
+            y_ptr = _dev(y, "y", bf, shape)
+        if state_out is None and want_state:
+            state_out = _new_states(S, H, N, r.device)
+            s_ptr = state_out.data_ptr()
+        else:
+            s_ptr = _dev(state_out, "state_out", torch.float32, (S, H, N, N))
+        args = [_dev(r, "r", bf), _dev(k, "k", bf, shape), _dev(v, "v", bf, shape), _dev(x, "x", bf, shape),
+                _dev(u2, "u2", bf, shape), _dev(state_in, "state_in", torch.float32, (S, H, N, N)),
+                s_ptr, y_ptr,
+                _dev(cu_seqlens, "cu_seqlens", torch.int32)]
         if split:
-            _ensure_workspace(S, int(max_seqlen), H, N, r.device)
+            _ensure_workspace(S, int(max_seqlen), H, N, r, stream)
         elif _workspace is not None:
             set_workspace(None)
         _check(lib.gf_wkv6_prefill_varlen_c2(*args, S, total_T, int(max_seqlen), H, N, _stream(stream)),
@@ -543,10 +558,11 @@ def step_c2(r, k, v, x, u2, state_in, state_out=None, y=None, stream=None):
     shape = r.shape
     B, H, N = shape
     bf = torch.bfloat16
-    if y is None:
-        y = torch.empty_like(r)
-    if state_out is None:
-        state_out = state_in if state_in is not None else _new_states(B, H, N, r.device)
+    with _HERE if stream is None else _on(r, stream, y is None or (state_out is None and state_in is None)):
+        if y is None:
+            y = torch.empty_like(r)
+        if state_out is None:
+            state_out = state_in if state_in is not None else _new_states(B, H, N, r.device)
     if _native is not None and stream is None:
         status = _native.step(r, k, v, x, u2, state_in, state_out, y, True)
         if status is not None:
@@ -555,7 +571,7 @@ def step_c2(r, k, v, x, u2, state_in, state_out=None, y=None, stream=None):
     args = [_dev(r, "r", bf), _dev(k, "k", bf, shape), _dev(v, "v", bf, shape), _dev(x, "x", bf, shape),
             _dev(u2, "u2", bf, shape), _dev(state_in, "state_in", torch.float32, (B, H, N, N)),
             _dev(state_out, "state_out", torch.float32, (B, H, N, N)), _dev(y, "y", bf, shape)]
-    with _on(r):
+    with _on(r, stream, False):
         _check(lib.gf_wkv6_step_c2(*args, B, H, N, _stream(stream)), "gf_wkv6_step_c2")
     return y, state_out
 
@@ -568,9 +584,9 @@ def sequence_summary(k, v, x, c2=False, out=None, stream=None):
     lib = load_library()
     B, T, H, N = k.shape
     bf = torch.bfloat16
-    if out is None:
-        out = torch.empty((B, H, SUMMARY_FLOATS), device=k.device, dtype=torch.float32)
-    with _on(k):
+    with _on(k, stream, out is None):
+        if out is None:
+            out = torch.empty((B, H, SUMMARY_FLOATS), device=k.device, dtype=torch.float32)
         _check(lib.gf_wkv6_sequence_summary(_dev(k, "k", bf), _dev(v, "v", bf, k.shape), _dev(x, "x", bf, k.shape),
                                             _dev(out, "summary", torch.float32, (B, H, SUMMARY_FLOATS)), B, T, H, N,
                                             1 if c2 else 0, _stream(stream)), "gf_wkv6_sequence_summary")
@@ -582,9 +598,9 @@ def fold_summaries(state_in, summaries, n_fold, state_out=None, stream=None):
     lib = load_library()
     P, B, H, F = summaries.shape
     assert F == SUMMARY_FLOATS and 0 <= n_fold <= P
-    if state_out is None:
-        state_out = torch.empty((B, H, 64, 64), device=summaries.device, dtype=torch.float32)
-    with _on(summaries):
+    with _on(summaries, stream, state_out is None):
+        if state_out is None:
+            state_out = torch.empty((B, H, 64, 64), device=summaries.device, dtype=torch.float32)
         _check(lib.gf_wkv6_fold_summaries(_dev(state_in, "state_in", torch.float32, (B, H, 64, 64)),
                                           _dev(summaries, "summaries", torch.float32), int(n_fold), B, H, 64,
                                           _dev(state_out, "state_out", torch.float32, (B, H, 64, 64)), _stream(stream)),
@@ -606,12 +622,12 @@ def layernorm_heads(y, gamma=None, beta=None, eps=1e-5, out=None, stream=None):
     H, N = y.shape[-2:]
     rows = y.numel() // (H * N) if H * N else 0
     sfx = _suffix(y.dtype)
-    if out is None:
-        out = torch.empty_like(y)
-        out_ptr = out.data_ptr()
-    else:
-        out_ptr = _dev(out, "out", y.dtype, y.shape)
-    with _on(y):
+    with _on(y, stream):
+        if out is None:
+            out = torch.empty_like(y)
+            out_ptr = out.data_ptr()
+        else:
+            out_ptr = _dev(out, "out", y.dtype, y.shape)
         gamma, beta = (None if t is None else t.reshape(H * N).contiguous() for t in (gamma, beta))       # (copies, where they are, live until the call)
         _check(getattr(lib, "gf_c2_layernorm" + sfx)(
             _dev(y, "y"), _dev(gamma, "gamma", torch.float32), _dev(beta, "beta", torch.float32), float(eps),
@@ -635,12 +651,12 @@ def key_compress(x, w_kd, out=None, stream=None):
     c_shape = c_shape[:-1] + (Dc,)
     rows = x.numel() // D if D else 0
     bf = torch.bfloat16
-    if out is None:
-        out = torch.empty(c_shape, device=x.device, dtype=bf)
-        c_ptr = out.data_ptr()
-    else:
-        c_ptr = _dev(out, "c", bf, c_shape)
-    with _on(x):
+    with _on(x, stream, out is None):
+        if out is None:
+            out = torch.empty(c_shape, device=x.device, dtype=bf)
+            c_ptr = out.data_ptr()
+        else:
+            c_ptr = _dev(out, "c", bf, c_shape)
         _check(lib.gf_gold_key_compress(_dev(x, "x", bf), _dev(w_kd, "w_kd", bf), c_ptr,
                                         rows, D, Dc, _stream(stream)), "gf_gold_key_compress")
     return out
@@ -671,12 +687,12 @@ def layernorm_heads_backward(y, dout, gamma=None, eps=1e-5, want_params=True, dy
     dt, f32 = y.dtype, torch.float32
     sfx = _suffix(dt)
     _one_device(y=y, dout=dout, gamma=gamma, dy=dy, workspace=workspace)
-    gamma = None if gamma is None else gamma.reshape(D).contiguous()       # (a copy, where it is one, lives until the call)
-    ins = [_dev(y, "y"), _dev(gamma, "gamma", f32), float(eps), _dev(dout, "dout", dt, y.shape)]
-    if dy is None:
-        dy = torch.empty_like(y)
-    dgamma = dbeta = ws = None
-    with _on(y):
+    with _on(y, stream):
+        gamma = None if gamma is None else gamma.reshape(D).contiguous()       # (a copy, where it is one, lives until the call)
+        ins = [_dev(y, "y"), _dev(gamma, "gamma", f32), float(eps), _dev(dout, "dout", dt, y.shape)]
+        if dy is None:
+            dy = torch.empty_like(y)
+        dgamma = dbeta = ws = None
         if want_params:
             dgamma, dbeta = torch.empty((2, D), device=y.device, dtype=f32).unbind()
             nbytes = int(lib.gf_c2_layernorm_backward_workspace_bytes(H, N))
@@ -725,9 +741,9 @@ def gated_linear(x, w, x2=None, w2=None, act="silu", out=None, stream=None):
     ptrs, code, (rows, K1, K2, F) = _gated_args(x, w, x2, w2, act)
     _one_device(x=x, w=w, x2=x2, w2=w2, out=out)
     shape = tuple(x.shape[:-1]) + (F,)
-    if out is None:
-        out = torch.empty(shape, device=x.device, dtype=torch.bfloat16)
-    with _on(x):
+    with _on(x, stream, out is None):
+        if out is None:
+            out = torch.empty(shape, device=x.device, dtype=torch.bfloat16)
         _check(lib.gf_gated_linear(*ptrs, code, _dev(out, "out", torch.bfloat16, shape), rows, K1, K2, F, _stream(stream)), "gf_gated_linear")
     return out
 
@@ -745,8 +761,8 @@ def gated_linear_backward(x, w, dy, x2=None, w2=None, act="silu", stream=None, w
             return res
     ptrs, code, (rows, K1, K2, F) = _gated_args(x, w, x2, w2, act)
     _one_device(x=x, w=w, x2=x2, w2=w2, dy=dy, workspace=workspace)
-    outs = [None if t is None else torch.empty_like(t) for t in (x, w, x2, w2)]
-    with _on(x):
+    with _on(x, stream):
+        outs = [None if t is None else torch.empty_like(t) for t in (x, w, x2, w2)]
         nbytes = int(lib.gf_gated_linear_backward_workspace_bytes(rows, K1, K2, F, w2 is not None and x2 is None))
         ws = workspace if workspace is not None and workspace.numel() >= nbytes else torch.empty(max(nbytes, 16), dtype=torch.uint8, device=x.device)
         _check(lib.gf_gated_linear_backward(*ptrs, code, _dev(dy, "dy", torch.bfloat16, tuple(x.shape[:-1]) + (F,)), *(_dev(t, "gradient") for t in outs),
@@ -779,8 +795,8 @@ def vocab_loss(x, w, targets, stream=None, workspace=None):
             return res
     ptrs, (rows, D, V), shape = _vocab_args(x, w, targets)
     _one_device(x=x, w=w, targets=targets, workspace=workspace)
-    loss, lse = (torch.empty(shape, device=x.device, dtype=torch.float32) for _ in range(2))
-    with _on(x):
+    with _on(x, stream):
+        loss, lse = (torch.empty(shape, device=x.device, dtype=torch.float32) for _ in range(2))
         nbytes = int(lib.gf_vocab_loss_workspace_bytes(rows, V))
         ws = workspace if workspace is not None and workspace.numel() >= nbytes else torch.empty(max(nbytes, 16), dtype=torch.uint8, device=x.device)
         _check(lib.gf_vocab_loss(*ptrs, loss.data_ptr(), lse.data_ptr(), rows, D, V, _dev(ws, "workspace"), ws.numel(), _stream(stream)), "gf_vocab_loss")
@@ -799,9 +815,9 @@ def vocab_loss_backward(x, w, targets, lse, dloss=None, stream=None, workspace=N
             return res
     ptrs, (rows, D, V), shape = _vocab_args(x, w, targets)
     _one_device(x=x, w=w, targets=targets, lse=lse, dloss=dloss, workspace=workspace)
-    dx, dw = torch.empty_like(x), torch.empty_like(w)
-    f32 = torch.float32
-    with _on(x):
+    with _on(x, stream):
+        dx, dw = torch.empty_like(x), torch.empty_like(w)
+        f32 = torch.float32
         nbytes = int(lib.gf_vocab_loss_backward_workspace_bytes(rows, D, V))
         ws = workspace if workspace is not None and workspace.numel() >= nbytes else torch.empty(max(nbytes, 16), dtype=torch.uint8, device=x.device)
         _check(lib.gf_vocab_loss_backward(*ptrs, _dev(lse, "lse", f32, shape), _dev(dloss, "dloss", f32, shape), dx.data_ptr(), dw.data_ptr(), rows, D, V,
@@ -817,9 +833,9 @@ def decay_logit(x, mu_x, A_d, B_d, lambda_d, A_w, B_w, lambda_w, x_prev=None, ou
     B, T, D = x.shape
     Rd, Rw = A_d.shape[1], A_w.shape[1]
     bf, f32 = torch.bfloat16, torch.float32
-    if out is None:
-        out = torch.empty_like(x)
-    with _on(x):
+    with _on(x, stream, out is None):
+        if out is None:
+            out = torch.empty_like(x)
         _check(lib.gf_c2_decay_logit(
             _dev(x, "x", bf), _dev(x_prev, "x_prev", bf, (B, D)), _dev(mu_x, "mu_x", f32, (D,)),
             _dev(A_d, "A_d", bf, (D, Rd)), _dev(B_d, "B_d", bf, (Rd, D)), _dev(lambda_d, "lambda_d", f32, (D,)),
@@ -862,24 +878,24 @@ def prefill_varlen(r, k, v, x, u, cu_seqlens, max_seqlen, state_in=None, state_o
     S = cu_seqlens.numel() - 1
     dt = r.dtype
     sfx = _suffix(dt)
-    if y is None:
-        y = torch.empty_like(r)
-        y_ptr = y.data_ptr()
-    else:
-        y_ptr = _dev(y, "y", dt, shape)
-    if state_out is None and want_state:
-        state_out = _new_states(S, H, N, r.device)
-        s_ptr = state_out.data_ptr()
-    else:
-        s_ptr = _dev(state_out, "state_out", torch.float32, (S, H, N, N))
-    args = [_dev(r, "r"), _dev(k, "k", dt, shape), _dev(v, "v", dt, shape),
-            _dev(x, "x", dt, shape), _dev(u, "u", torch.float32, (H, N)),
-            _dev(state_in, "state_in", torch.float32, (S, H, N, N)),
-            s_ptr, y_ptr,
-            _dev(cu_seqlens, "cu_seqlens", torch.int32)]
-    with _on(r):
+    with _on(r, stream, y is None or (state_out is None and want_state)):
+        if y is None:
+            y = torch.empty_like(r)
+            y_ptr = y.data_ptr()
+        else:
+            y_ptr = _dev(y, "y", dt, shape)
+        if state_out is None and want_state:
+            state_out = _new_states(S, H, N, r.device)
+            s_ptr = state_out.data_ptr()
+        else:
+            s_ptr = _dev(state_out, "state_out", torch.float32, (S, H, N, N))
+        args = [_dev(r, "r"), _dev(k, "k", dt, shape), _dev(v, "v", dt, shape),
+                _dev(x, "x", dt, shape), _dev(u, "u", torch.float32, (H, N)),
+                _dev(state_in, "state_in", torch.float32, (S, H, N, N)),
+                s_ptr, y_ptr,
+                _dev(cu_seqlens, "cu_seqlens", torch.int32)]
         if sfx == "" and split:
-            _ensure_workspace(S, int(max_seqlen), H, N, r.device)
+            _ensure_workspace(S, int(max_seqlen), H, N, r, stream)
         elif not split and _workspace is not None:
             set_workspace(None)
         _check(getattr(lib, "gf_wkv6_prefill_varlen" + sfx)(*args, S, total_T, int(max_seqlen), H, N, _stream(stream)),
@@ -895,10 +911,11 @@ def step(r, k, v, x, u, state_in, state_out=None, y=None, stream=None):
     B, H, N = shape
     dt = r.dtype
     sfx = _suffix(dt)
-    if y is None:
-        y = torch.empty_like(r)
-    if state_out is None:
-        state_out = state_in if state_in is not None else _new_states(B, H, N, r.device)
+    with _HERE if stream is None else _on(r, stream, y is None or (state_out is None and state_in is None)):
+        if y is None:
+            y = torch.empty_like(r)
+        if state_out is None:
+            state_out = state_in if state_in is not None else _new_states(B, H, N, r.device)
     if _native is not None and stream is None:
         status = _native.step(r, k, v, x, u, state_in, state_out, y, False)
         if status is not None:
@@ -908,7 +925,7 @@ def step(r, k, v, x, u, state_in, state_out=None, y=None, stream=None):
             _dev(x, "x", dt, shape), _dev(u, "u", torch.float32, (H, N)),
             _dev(state_in, "state_in", torch.float32, (B, H, N, N)),
             _dev(state_out, "state_out", torch.float32, (B, H, N, N)), _dev(y, "y", dt, shape)]
-    with _on(r):
+    with _on(r, stream, False):
         _check(getattr(lib, "gf_wkv6_step" + sfx)(*args, B, H, N, _stream(stream)), "gf_wkv6_step" + sfx)
     return y, state_out
 
@@ -920,15 +937,16 @@ def bind_step(r, k, v, x, u, state, y=None, stream=None):
     lib = load_library()
     B, H, N = r.shape
     sfx = _suffix(r.dtype)
-    if y is None:
-        y = torch.empty_like(r)
-    args = [_dev(r, "r"), _dev(k, "k", r.dtype, r.shape), _dev(v, "v", r.dtype, r.shape),
-            _dev(x, "x", r.dtype, r.shape), _dev(u, "u", torch.float32, (H, N)),
-            _dev(state, "state", torch.float32, (B, H, N, N)), _dev(state, "state", torch.float32, (B, H, N, N)),
-            _dev(y, "y", r.dtype, r.shape), B, H, N, _stream(stream)]
+    with _on(r, stream):
+        if y is None:
+            y = torch.empty_like(r)
+        args = [_dev(r, "r"), _dev(k, "k", r.dtype, r.shape), _dev(v, "v", r.dtype, r.shape),
+                _dev(x, "x", r.dtype, r.shape), _dev(u, "u", torch.float32, (H, N)),
+                _dev(state, "state", torch.float32, (B, H, N, N)), _dev(state, "state", torch.float32, (B, H, N, N)),
+                _dev(y, "y", r.dtype, r.shape), B, H, N, _stream(stream)]
     fn = getattr(lib, "gf_wkv6_step" + sfx)
     keep = (r, k, v, x, u, state, y)                 # the bound buffers must outlive the callable
-    index = r.device.index
+    index = r.get_device()
 
     def call():
         if torch.cuda.current_device() != index:
