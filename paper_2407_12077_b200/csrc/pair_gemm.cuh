@@ -803,8 +803,9 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
                     }
                 }
             } else if constexpr (EPI == EPI_LSE) {
-                // a warp takes half of the tile's columns.  exp is taken of differences to a reference, the largest value so far (0
-                // instead of an infinite one: the sum is then infinite, or zero, by itself); a NaN reaches the sum through its own exponential
+                // a warp takes half of the tile's columns.  exp is taken of differences to a reference, the largest value so far, which stays
+                // finite: FLT_MAX for +inf (the sum is infinite by itself, and no later reference scales it down), -FLT_MAX where all are
+                // -inf (the sum is zero, and any other reference is larger); a NaN reaches the sum through its own exponential
                 float ref = -FLT_MAX, sum = 0.f;
                 for (int c = HW * part; c < HW * part + HW; c += 64) {
                     const int col = tn * BN + c;
@@ -829,9 +830,7 @@ __global__ void __launch_bounds__(THREADS, 1) pair_gemm_kernel(const __grid_cons
 #pragma unroll
                         for (int j = 0; j < 32; ++j) t4[j & 3] = fmaxf(t4[j & 3], v[half][j]);
                     }
-                    float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
-                    top = c == HW * part ? top : fmaxf(top, ref);
-                    top = fabsf(top) < INFINITY ? top : 0.f;
+                    const float top = fminf(fmaxf(fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])), ref), FLT_MAX);
                     float2 s2[4] = {make_float2(sum * ex2((ref - top) * LOG2E), 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {

@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const float2* __rest
     asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
     const int share = threadIdx.x / ROWS, r = threadIdx.x % ROWS, row = blockIdx.x * ROWS + r;
     float ref = -INFINITY, sum = 0.f;
-    // (references are finite, so a first one's factor below is exp(-inf) = 0)
+    // (references are finite, so a first one's factor below is exp(-inf) = 0; an infinite sum's is FLT_MAX, so its own factor is 1)
     auto join = [&](float2 o) {
         const float top = fmaxf(ref, o.x);
         sum = sum * __expf(ref - top) + o.y * __expf(o.x - top);
