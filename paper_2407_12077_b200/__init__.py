@@ -236,6 +236,7 @@ def _suffix(dtype) -> str:
 
 
 _workspace = None            # the registered scratch tensor is kept alive here
+_workspace_streams = set()   # raw handles of the streams that the caching allocator knows it to be used on
 
 
 def workspace_bytes(B, T, H, N=64) -> int:
@@ -253,19 +254,29 @@ def split_plan(B, T, H, n_sm, scratch_cap=0, N=64):
 
 
 def set_workspace(buf: torch.Tensor | None) -> None:
-    """gf_wkv6_set_workspace: register a CUDA byte tensor as the library's scratch (None unregisters)."""
+    """gf_wkv6_set_workspace: register a CUDA byte tensor as the library's scratch (None unregisters).  The one before, if nothing else
+    holds it, goes back to torch's allocator, which keeps it until the calls on every stream that used it are done."""
     global _workspace
     lib = load_library()
+    if _native is not None:                      # (nothing, until the stream of a call is noted)
+        _native.set_workspace(0, 0, 0)
     if buf is None:
-        if _native is not None:
-            _native.set_workspace(0, 0)
         _check(lib.gf_wkv6_set_workspace(None, 0), "gf_wkv6_set_workspace")
     else:
         nbytes = buf.numel() * buf.element_size()
         _check(lib.gf_wkv6_set_workspace(_dev(buf, "workspace"), nbytes), "gf_wkv6_set_workspace")
-        if _native is not None:                  # (as _ensure_workspace sees it)
-            _native.set_workspace(buf.get_device(), buf.numel())
+    _workspace_streams.clear()
     _workspace = buf
+
+
+def _note_workspace_use(stream) -> None:
+    """The registered scratch is used on `stream` (of the current device): the allocator must not hand it on while that stream needs it."""
+    handle = _stream(stream)
+    if handle not in _workspace_streams:
+        _workspace.record_stream(torch.cuda.ExternalStream(handle, device=_workspace.device))
+        _workspace_streams.add(handle)
+    if _native is not None:                      # (as _ensure_workspace sees it, for further calls on this stream)
+        _native.set_workspace(_workspace.get_device(), _workspace.numel(), handle)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -282,6 +293,8 @@ def _ensure_workspace(B, T, H, N, r, stream) -> None:
     if need > have:
         with _on(r, stream):
             set_workspace(torch.empty(need, dtype=torch.uint8, device=device))
+    if need > 0:
+        _note_workspace_use(stream)
 
 
 def last_device_status(stream=None) -> None:

@@ -38,8 +38,10 @@ typedef size_t (*LossGradBytesFn)(long long, int, long long);
 enum { PREFILL, PREFILL_F32, PREFILL_C2, VARLEN, VARLEN_F32, VARLEN_C2, STEP, STEP_F32, STEP_C2, LAYERNORM, LAYERNORM_F32, KEY_COMPRESS, WORKSPACE_BYTES,
        NORM_GRAD, NORM_GRAD_F32, NORM_GRAD_BYTES, GATED, GATED_GRAD, GATED_GRAD_BYTES, LOSS, LOSS_BYTES, LOSS_GRAD, LOSS_GRAD_BYTES, N_FNS };
 void* fns[N_FNS];
-// the scratch that is registered with the library: the device it is on (upper 16 bits), its size in bytes
+// the scratch that is registered with the library: the device it is on (upper 16 bits), its size in bytes; a stream that torch's allocator
+// knows it to be used on
 std::atomic<uint64_t> workspace{0};
+std::atomic<void*> workspace_stream{nullptr};
 
 // no torch-function or dispatch mode is active: allocations here mean what they mean in Python
 bool plain_mode()
@@ -109,12 +111,13 @@ template <typename F> PyObject* guarded(F&& f)
     }
 }
 
+// (a call on another stream than the noted one goes through Python, which notes it)
 bool workspace_suffices(int dev, int B, int T, int H)
 {
     const size_t need = reinterpret_cast<WorkspaceBytesFn>(fns[WORKSPACE_BYTES])(B, T, H, 64);
     if (need == 0) return true;
     const uint64_t w = workspace.load(std::memory_order_acquire);
-    return (int)(w >> 48) == dev && (w & ((1ull << 48) - 1)) >= need;
+    return (int)(w >> 48) == dev && (w & ((1ull << 48) - 1)) >= need && workspace_stream.load(std::memory_order_acquire) == (void*)c10::cuda::getCurrentCUDAStream().stream();
 }
 
 // prefill(r, k, v, x, u or u2 (or None), state_in or None, c2)
@@ -482,12 +485,14 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
-// set_workspace(device index, bytes): what is registered with the library now (0 bytes: nothing)
+// set_workspace(device index, bytes, stream): what is registered with the library now (0 bytes: nothing), and a stream it is noted to be used on
 PyObject* set_workspace(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-    if (n != 2) { PyErr_SetString(PyExc_TypeError, "set_workspace(device, bytes)"); return nullptr; }
+    if (n != 3) { PyErr_SetString(PyExc_TypeError, "set_workspace(device, bytes, stream)"); return nullptr; }
     const unsigned long long dev = PyLong_AsUnsignedLongLong(a[0]), bytes = PyLong_AsUnsignedLongLong(a[1]);
+    void* stream = PyLong_AsVoidPtr(a[2]);
     if (PyErr_Occurred()) return nullptr;
+    workspace_stream.store(stream, std::memory_order_release);
     workspace.store(dev << 48 | (bytes & ((1ull << 48) - 1)), std::memory_order_release);
     Py_RETURN_NONE;
 }

@@ -165,3 +165,23 @@ def test_a_stream_of_another_device_is_refused(host):
         with pytest.raises(ValueError, match="device"):
             call(there)
     assert not host.calls and host.stream == CURRENT
+
+
+def test_scratch_is_noted_on_every_stream_that_uses_it(host):
+    """The registered scratch outlives calls on several streams: torch's allocator is told of each before the scratch can be dropped."""
+    d, u = torch.zeros(1, 8, 2, 64, dtype=BF), torch.zeros(2, 64)
+    gf.prefill(d, d, d, d, u)
+    first = gf._workspace.data_ptr()
+    gf.prefill(d, d, d, d, u, stream=Side())
+    gf.prefill_c2(d, d, d, d, stream=SIDE)
+    gf.prefill(d, d, d, d, u)
+    assert host.recorded == [(first, CURRENT), (first, SIDE)]
+    mine = torch.zeros(1 << 13, dtype=torch.uint8)
+    gf.set_workspace(mine)                           # a buffer of the caller's, wherever it was made
+    gf.prefill(d, d, d, d, u, stream=SIDE)
+    assert host.recorded[2:] == [(mine.data_ptr(), SIDE)]
+    gf.set_workspace(None)
+    gf.prefill(d, d, d, d, u, stream=SIDE)
+    assert len(host.recorded) == 4 and host.recorded[3][1] == SIDE
+    gf.prefill(d.float(), d.float(), d.float(), d.float(), u, stream=Side(55))      # (no scratch in fp32)
+    assert len(host.recorded) == 4

@@ -88,3 +88,28 @@ def test_two_streams_at_a_time():
             for n in w:
                 equal(g[n], w[n], n)
     gf.last_device_status()
+
+
+@pytest.mark.parametrize("how", ["stream=", "context"])
+def test_dropped_scratch_is_not_handed_on_while_another_stream_uses_it(how):
+    """A prefill that splits: scratch made on the current stream, used on another one, replaced and dropped while that one still runs."""
+    d = synth.make_dense(1, 4096, 4, 64, "bf16", seed=3, device=DEV, state_std=0.1)
+    need = gf.workspace_bytes(1, 4096, 4)
+    assert need > 0
+    gf.set_workspace(None)
+    want = gf.prefill(d.r, d.k, d.v, d.x, d.u, d.state_in)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        gf.set_workspace(torch.empty(need, dtype=torch.uint8, device=DEV))
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(4_000_000)
+            got = gf.prefill(d.r, d.k, d.v, d.x, d.u, d.state_in) if how == "context" else None
+        if got is None:
+            got = gf.prefill(d.r, d.k, d.v, d.x, d.u, d.state_in, stream=side)
+        gf.set_workspace(None)
+        held = [torch.full((need,), 255, dtype=torch.uint8, device=DEV) for _ in range(3)]
+        torch.cuda.synchronize()
+        gf.last_device_status(side)
+        equal(got, want, how)
+        del held
