@@ -175,6 +175,16 @@ def _stream(stream) -> int:
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _torch_stream(stream, index: int):
+    """The torch.cuda.Stream that _stream(stream) is the handle of, on device `index`."""
+    if stream is None:
+        return torch.cuda.current_stream(index)
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = _stream(stream)               # (ExternalStream(0) would be a new stream instead of the default one)
+    return torch.cuda.ExternalStream(handle, device=index) if handle else torch.cuda.default_stream(index)
+
+
 class _Here:
     """The device guard of a call whose tensors already live on the current device: nothing to do."""
 
@@ -203,7 +213,7 @@ def _on(t: torch.Tensor, stream=None, makes=True):
         if isinstance(stream, torch.cuda.Stream) and stream.device_index != index:
             raise ValueError(f"stream on device {stream.device_index}, tensors on device {index}")
         if makes and (index != torch.cuda.current_device() or _stream(stream) != torch._C._cuda_getCurrentRawStream(index)):
-            return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream), device=index))
+            return torch.cuda.stream(_torch_stream(stream, index))
     return _HERE if index == torch.cuda.current_device() else torch.cuda.device(index)
 
 
@@ -273,7 +283,7 @@ def _note_workspace_use(stream) -> None:
     """The registered scratch is used on `stream` (of the current device): the allocator must not hand it on while that stream needs it."""
     handle = _stream(stream)
     if handle not in _workspace_streams:
-        _workspace.record_stream(torch.cuda.ExternalStream(handle, device=_workspace.device))
+        _workspace.record_stream(_torch_stream(stream, _workspace.get_device()))
         _workspace_streams.add(handle)
     if _native is not None:                      # (as _ensure_workspace sees it, for further calls on this stream)
         _native.set_workspace(_workspace.get_device(), _workspace.numel(), handle)

@@ -185,3 +185,29 @@ def test_scratch_is_noted_on_every_stream_that_uses_it(host):
     assert len(host.recorded) == 4 and host.recorded[3][1] == SIDE
     gf.prefill(d.float(), d.float(), d.float(), d.float(), u, stream=Side(55))      # (no scratch in fp32)
     assert len(host.recorded) == 4
+
+
+@pytest.fixture
+def default_stream(host, monkeypatch):
+    """torch.cuda.ExternalStream(0) is a stream from torch's pool; handle 0 is the default stream."""
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: Side(handle or 1000))
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: Side(0))
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_handle_zero_is_the_default_stream(host, default_stream, name):
+    call = run_all()[name]
+    with Watch(host):
+        call(0)
+    made = [m for m in host.made if name != "fold_summaries" or "zeros" not in m[0]]
+    assert made and all(stream == 0 for _, stream in made), made
+    assert host.calls and all(handle == 0 for _, handle, _ in host.calls)
+
+
+def test_scratch_is_noted_on_the_default_stream(host, default_stream):
+    d, u = torch.zeros(1, 8, 2, 64, dtype=BF), torch.zeros(2, 64)
+    gf.set_workspace(torch.zeros(1 << 13, dtype=torch.uint8))
+    gf.prefill(d, d, d, d, u, stream=0)
+    host.stream = 0                                  # (the current one from here on)
+    gf.prefill(d, d, d, d, u)
+    assert [handle for _, handle in host.recorded] == [0]

@@ -113,3 +113,20 @@ def test_dropped_scratch_is_not_handed_on_while_another_stream_uses_it(how):
         gf.last_device_status(side)
         equal(got, want, how)
         del held
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_default_stream_by_its_handle_while_another_one_is_current(name):
+    call = calls(make(2))[name]
+    want = call(None)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        torch.cuda._sleep(4_000_000)
+        with torch.cuda.stream(side):
+            got = call(0)
+            held = scribble()
+        torch.cuda.synchronize()
+        gf.last_device_status()
+        equal(got, want, name)
+        del held, got
