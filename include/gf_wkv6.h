@@ -469,7 +469,7 @@ GF_API size_t gf_c2_layernorm_backward_workspace_bytes(int H, int N);
  *   x    DEVICE bf16 [rows][K1]        w    DEVICE bf16 [K1][F] row-major
  *   w2   DEVICE bf16 [K2][F], or NULL: no second factor (then x2 is NULL and K2 is 0)
  *   x2   DEVICE bf16 [rows][K2], or NULL: x itself (then K2 is K1)
- *   y    DEVICE bf16 [rows][F], written; must not be one of the inputs
+ *   y    DEVICE bf16 [rows][F], written; must not overlap an input
  *   act  gf_act_t: sigmoid; relu(a)^2; silu, a sigmoid(a); gelu, a Phi(a) with the normal distribution Phi
  * Both products on the tensor cores with fp32 accumulation, activation and product in fp32, one rounding to bf16.  K1, K2 and
  * F are multiples of 8 (GF_ERR_UNSUPPORTED otherwise); pointers 16-byte aligned; rows = 0 is a no-op.  Enqueues one kernel on
@@ -482,13 +482,13 @@ GF_API gf_status_t gf_gated_linear(const void *x, const void *w, const void *x2,
  *     dx = da W^T,   dw = x^T da,   dx2 = db W2^T,   dw2 = x2^T db;   with x2 = NULL, dx = da W^T + db W2^T.
  *   x, w, x2, w2, act, sizes   as for gf_gated_linear;   dy  DEVICE bf16 [rows][F]
  *   dx [rows][K1], dw [K1][F], dx2 [rows][K2], dw2 [K2][F]   DEVICE bf16, written; dw2 is NULL without w2, dx2 without x2; none may
- *                 be an input or another output
+ *                 overlap an input or another output
  *   workspace     DEVICE, gf_gated_linear_backward_workspace_bytes(rows,K1,K2,F,same) bytes, 16-byte aligned, with K2 = 0 without w2 and
  *                 same = 1 where x2 is NULL for x (da and db, and fp32 sums of products that are cut along their
  *                 contraction index, on the current device); GF_ERR_WORKSPACE if absent or too small
- * relu^2 has derivative 0 at 0.  da and db are rounded to bf16 (they are operands of the second products; of up to 128 rows what the
- * rounding leaves is multiplied as well), sums are fp32, results
- * rounded once, in an order that the sizes and the GPU alone decide.  rows = 0 writes zeros to dw and dw2.  Enqueues two kernels on
+ * relu^2 has derivative 0 at 0.  da and db are rounded to bf16 (they are operands of the second products), each off by half a step of its own
+ * value; of up to 128 rows what the rounding leaves is multiplied as well (0 times an infinite weight, so NaN there where the
+ * formula has an infinity).  Sums are fp32, results rounded once, in an order that the sizes and the GPU alone decide.  rows = 0 writes zeros to dw and dw2.  Enqueues two kernels on
  * `stream` (three where a product is cut), allocates nothing, does not synchronise. */
 GF_API gf_status_t gf_gated_linear_backward(const void *x, const void *w, const void *x2, const void *w2, int act,
                                      const void *dy, void *dx, void *dw, void *dx2, void *dw2, long long rows, int K1,
@@ -513,11 +513,12 @@ GF_API size_t gf_vocab_loss_workspace_bytes(long long rows, long long V);
 /* Gradient of gf_vocab_loss: with P[t][v] = (exp(z[t][v] - lse[t]) - [v is the target of t]) dloss[t], and 0 in rows without a
  * target,    dx = P W,   dw = P^T x.
  *   x, w, targets, sizes   as for gf_vocab_loss, lse what it wrote;   dloss  DEVICE fp32 [rows] (alignment as lse), or NULL for 1 in every row
- *   dx [rows][D], dw [V][D]   DEVICE bf16, written; neither may be an input
+ *   dx [rows][D], dw [V][D]   DEVICE bf16, written; neither may overlap an input or the other
  *   workspace  DEVICE, gf_vocab_loss_backward_workspace_bytes(rows,D,V) bytes, 16-byte aligned; GF_ERR_WORKSPACE if absent or
  *              too small (256 MB for a piece of P, 2 KB per row at least, twice that for up to 128 rows; fp32 sums of dx where the vocabulary takes several pieces, and of
  *              products that are cut along their contraction index, 256 MB at most)
- * P is rounded to bf16 (it is an operand of both products; of up to 128 rows what the rounding leaves is multiplied as well), sums are fp32, results rounded once, in an order that the sizes and the GPU
+ * P is rounded to bf16 (it is an operand of both products), each value off by half a step of its own; of up to 128 rows what the rounding leaves is
+ * multiplied as well (`rows` decides, not how many of them have a target).  Sums are fp32, results rounded once, in an order that the sizes and the GPU
  * alone decide.  rows = 0 writes zeros to dw.  Enqueues two kernels per piece of the vocabulary on `stream` (three where a product is
  * cut), allocates nothing, does not synchronise. */
 GF_API gf_status_t gf_vocab_loss_backward(const void *x, const void *w, const int64_t *targets, const float *lse,

@@ -313,7 +313,7 @@ def last_device_status(stream=None) -> None:
 
 
 def set_wait_limit(microseconds: int) -> None:
-    """gf_wkv6_set_wait_limit: bound of every device-side wait of later launches (0: the default of 2 s)."""
+    """gf_wkv6_set_wait_limit: bound of every device-side wait of the recurrence's later launches (0: the default of 2 s)."""
     _check(load_library().gf_wkv6_set_wait_limit(int(microseconds)), "gf_wkv6_set_wait_limit")
 
 

@@ -318,7 +318,7 @@ __device__ __forceinline__ Tile tile_at(const GemmParams& p, int tile, int share
         i -= t.slice * places;
     }
     const uint32_t of = g.slices * shares, nth = t.slice + share;
-    t.lo = (int)((uint32_t)g.steps * nth / of);       // (steps <= 2^26, of <= 32)
+    t.lo = (int)((uint32_t)g.steps * nth / of);       // (steps <= 2^27 - 16, four segments of a tensor's longest side; of <= 32)
     t.hi = (int)((uint32_t)g.steps * (nth + 1) / of);
     // bands of eight tiles along m, column by column: the tiles that run at one time share few rows of A and of B
     const int per = 8 * g.tiles_n, band = (int)((__umulhi((uint32_t)i, g.per_mul) + (uint32_t)i) >> g.per_shift), rest = i - band * per;
@@ -1049,10 +1049,14 @@ inline bool launch(const Launch& l, const GemmParams& p, cudaStream_t st, std::a
 }
 
 // ---------------------------------------------------------------- several products in one launch (a gradient's)
-// A gradient's first operand (da, db, P) is rounded to bf16.  Over many rows the roundings average out to about the result's own (2.3e-3 of the
-// result's norm in all, the result's rounding alone being 1.7e-3); with few rows a few large values carry the result, and the error with
-// them (up to 2.7e-3).  There what the rounding leaves is kept too, in a second bf16 tensor, and multiplied as well: such calls wait for
-// launches and weights, not for products (24 rows, 424 deep -> 2072, gated: 17 us -> 25; 20 rows, 1704 deep, over 14752 entries: 64 -> 76).
+// A gradient's first operand (da, db, P) is rounded to bf16: 2.2e-3 to 2.4e-3 of the result's norm in all, whatever the number of rows (1 to 1024
+// measured), the result's own rounding being 1.7e-3 of it.  That is what many roundings average to; where one row or two carry a result,
+// a few of them decide (1.5e-3 to 3.2e-3 measured).  Up to REST_ROWS rows what the rounding leaves is kept too, in a second bf16 tensor, and
+// multiplied as well: 1.6e-3 to 1.8e-3.  Such a call is one tile of rows and waits for launches and weights; it pays 6 to 20 us (us without
+// and with, 16 and 128 rows: gated 424 -> 2072 19, 28 and 23, 35; 768 -> 2688 27, 32 and 29, 36; the loss, 768 deep over 40011 entries, 55, 67 and
+// 61, 81).  With more rows the products count, and the price grows with them (512 and 1024 rows: 768 -> 2688 31, 49 and 40, 69; the loss
+// 111, 173 and 163, 279).  The rule goes by the tensors' rows: how many of them have a target is known on the device alone, so a
+// batch of more rows that is masked but for a few has the error of one rounding (1024 rows, one target: up to 3.2e-3).
 constexpr long long REST_ROWS = 128;
 inline bool keep_rests(long long rows) { return rows <= REST_ROWS; }
 // Time of 64 contraction indices, in units of 1/30 us.  An SM takes in 64 bytes per cycle: the 32 KB of its share of a pair's 256 x 256 products
